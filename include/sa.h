@@ -87,7 +87,10 @@ typedef enum { SA_OP_FWD = 0, SA_OP_BWD = 1, SA_OP_GATED_FWD = 2, SA_OP_GATED_BW
                SA_OP_DUAL_PATH_BWD = 7,        /* sa_dual_path_bwd                */
                SA_OP_SAMPLE_PERM = 8,          /* sa_sample_perm, O(n) path       */
                SA_OP_DECODE = 9,               /* sa_decode_fwd                   */
-               SA_OP_BWD_ROPE = 10             /* sa_bwd_rope                     */
+               SA_OP_BWD_ROPE = 10,            /* sa_bwd_rope                     */
+               SA_OP_CACHE4_DECODE = 11,       /* sa_cache4_decode_fwd (sa_cache4_workspace_bytes) */
+               SA_OP_PAGES_EXTEND = 12,        /* sa_pages_extend  (sa_cache4_workspace_bytes) */
+               SA_OP_PAGES_COMPACT = 13        /* sa_pages_compact (sa_cache4_workspace_bytes) */
 } sa_op;
 
 const char* sa_status_string(sa_status s);
@@ -278,6 +281,96 @@ sa_status sa_bwd(const sa_desc* sa, const sa_desc* swa,
                  const void* dY,
                  void* dQ, void* dK, void* dV, void* dgate_sa, void* dgate_swa,
                  void* ws, size_t ws_bytes, void* stream);
+
+/* ---- K/V caches held in 4 bits and in pages ------------------------------------------------------------------------
+ * For the decoding of Sec. 4.2: a quarter of the bytes of the dense bf16 caches of sa_decode_fwd, and sequences that
+ * take memory by the rows they hold and may share it.
+ *
+ * Format (the FP4 of the OCP Microscaling formats): an element is E2M1, sign and magnitude 0 .5 1 1.5 2 3 4 6 (codes
+ * 0..7); 32 neighbouring elements of a row share a power of two 2^e, held as the byte e + 127.  With amax the largest
+ * magnitude of the 32, e = floor(log2 amax) - 2, and one more if amax / 2^e > 7 (8 is then as near as 6 or nearer); at
+ * least -125, so that every value held is a normal bf16 number and is exact in both dtypes.  Elements are rounded to the nearest, ties to the even
+ * code, those above 6 to 6.  A row whose K or V has an infinity or NaN in a KV head is held as such in that head (scale
+ * bytes of K 255, of V 2, codes 0): it reads back as NaN in K and V and makes Y and LSE of every query that sees it NaN; queries that do
+ * not see it are as if it were not there.
+ *
+ * Pool: [layers][pages][Hkv][page_rows/32] tiles of 34 d bytes, 16-byte aligned; a tile is 32 rows of one head:
+ *   K codes  [row 32][d/2]                                        element 2x in the low half of byte x
+ *   V codes  [(row % 16) / 4][x 16][row / 16][row % 4][d/32]      bytes x d/32 .. of the row
+ *   K scales [d/32][row % 16][row / 16],  V scales [d/32][(row % 16) / 4][row / 16][row % 4]
+ * (rows and columns lie as the lanes of the matrix instructions take them.)  A position p of sequence b is row
+ * p % page_rows of page table[b][p / page_rows]; table is int32 [B, max_pages], shared by the layers.  An entry outside
+ * 0..pages-1 is a page that is not there: rows written to it are dropped, its rows read back as zeros and are not seen by attention.
+ * Nothing outside the pool is touched whatever the tables hold. */
+typedef struct {
+  int32_t B, Hq, Hkv, d;  /* sequences, heads (Hq % Hkv == 0), d in {64,128}                        */
+  int32_t page_rows;      /* rows of a page: a power of two, 32 .. 1024                             */
+  int32_t pages;          /* pages of a layer                                                       */
+  int32_t max_pages;      /* table entries of a sequence; max_pages * page_rows <= 2^30             */
+  int32_t layers;         /* layers of the pool, for the calls that move pages (sa_pages_*)         */
+  int32_t dtype;          /* sa_dtype of q, Y and of the K and V rows written and read              */
+  float scale;            /* softmax scale; <= 0 selects 1/sqrt(d) (Eq. 1)                          */
+} sa_cache4_desc;         /* SA_ERR_SHAPE beyond: B*max_pages < 2^31, pages*Hkv*page_rows/32 < 2^31 */
+
+/* Bytes of the pool, of all layers (0 for an invalid descriptor). */
+size_t sa_cache4_pool_bytes(const sa_cache4_desc* desc);
+
+/* Bytes of device workspace of SA_OP_CACHE4_DECODE (T tokens), SA_OP_PAGES_EXTEND or SA_OP_PAGES_COMPACT (T unused);
+ * 0 for an invalid descriptor or T < 1. */
+size_t sa_cache4_workspace_bytes(const sa_cache4_desc* desc, int op, int32_t T);
+
+/* Writes rows into the cache of one layer.  K, V [B,Hkv,T,d] (desc->dtype); row t < counts[b] of sequence b goes to
+ * position starts[b] + t.  starts, counts: int32 [B], device; starts NULL: 0, counts NULL: T; a count is clamped to 0..T,
+ * positions outside 0..max_pages*page_rows-1 are dropped.  Every other row of the cache stays as it is.
+ * `pool` is the layer's part.  Sequences that share a page must not write to it (sa_pages_extend sees to that). */
+sa_status sa_cache4_write(const sa_cache4_desc* desc, const void* K, const void* V, int32_t T, const int32_t* starts,
+                          const int32_t* counts, const int32_t* table, void* pool, void* stream);
+
+/* The reverse: row t < counts[b] of K, V [B,Hkv,T,d] becomes what the cache holds at position starts[b] + t (exact in
+ * either dtype; zeros where there is no such position or page): what sa_fwd takes when a prompt follows rows that are cached.  Rows
+ * t >= counts[b] of K and V stay as they are. */
+sa_status sa_cache4_read(const sa_cache4_desc* desc, const void* pool, const int32_t* table, int32_t T,
+                         const int32_t* starts, const int32_t* counts, void* K, void* V, void* stream);
+
+/* sa_decode_fwd over the cache of one layer, for the last T tokens of every sequence at once (T = 1: a generated token;
+ * more: drafted tokens, a follow-up prompt).  q, Y [B,Hq,T,d], LSE [B,Hq,T] (fp32, may be NULL).  lens [B] (int32,
+ * device): rows of each sequence, the T tokens' own included, clamped to 0..max_len on the device; max_len (host,
+ * 1 <= max_len <= max_pages*page_rows) sizes the launch.  Token t sees the positions <= lens[b] - T + t whose pages are there;
+ * one that sees none gets Y = 0 and LSE = -inf.  B*Hq*T < 2^31 (SA_ERR_SHAPE).
+ * Scores, softmax and sums are fp32; K and V enter exactly, probabilities with 17 bits (bf16) or 24 (fp32).
+ * ws: sa_cache4_workspace_bytes(desc, SA_OP_CACHE4_DECODE, T) bytes (may be NULL if that is 0). */
+sa_status sa_cache4_decode_fwd(const sa_cache4_desc* desc, const void* q, int32_t T, const void* pool,
+                               const int32_t* table, const int32_t* lens, int32_t max_len, void* Y, float* LSE,
+                               void* ws, size_t ws_bytes, void* stream);
+
+/* Page tables.  refs [pages] (int32, device) counts the table entries that name each page (a caller may count more, to hold a page);
+ * a page is free if its count is <= 0.  All of table, lens, refs, info are device memory; the host never waits.
+ *
+ * sa_pages_fork deals the sequences anew: sequence b becomes what parents[b] (int32 [B]) was before the call; parents[b] == b stays,
+ * a value outside 0..B-1 leaves it empty (which gives its pages back).  Of a parent the entries of its lens rows are
+ * taken over, the rest is -1; pages are shared, not copied.  Writes table_out [B,max_pages], lens_out [B] and refs_out;
+ * table_out and lens_out must not overlap their inputs (SA_ERR_UNSUPPORTED), refs_out may be refs.
+ *
+ * sa_pages_free keeps the pages of the first keep[b] rows (clamped to 0..) of every sequence; the entries behind them become -1.
+ *
+ * sa_pages_extend makes room for rows lens[b] .. lens[b] + add[b] - 1 (up to the capacity; add <= 0: none): entries that
+ * these rows touch and that are not there get free pages, those whose page is shared (count > 1) get a page of their own, into which
+ * the shared page is copied, in all layers, if rows below lens[b] lie in it.  Pages are dealt lowest first, in the
+ * order of b and position.  info[0] = pages taken; if too few are free nothing is changed, info[0] = 0 and
+ * info[1] = pages that lack (0 otherwise).  All sequences are judged by the counts before the call.
+ *
+ * sa_pages_compact moves pages in use to the front: with U pages in use, the highest of them goes to the lowest free page,
+ * and so on until all lie below U or max_moves pages have moved.  Pages move in all layers; table entries and counts
+ * follow (table_out, refs_out: the inputs, or apart from them; SA_ERR_UNSUPPORTED if they overlap otherwise).
+ * info[0] = U, info[1] = pages moved.  A page with a count that no entry names moves too. */
+sa_status sa_pages_fork(const sa_cache4_desc* desc, const int32_t* parents, const int32_t* table, const int32_t* lens,
+                        const int32_t* refs, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, void* stream);
+sa_status sa_pages_free(const sa_cache4_desc* desc, const int32_t* keep, int32_t* table, int32_t* refs, void* stream);
+sa_status sa_pages_extend(const sa_cache4_desc* desc, const int32_t* lens, const int32_t* add, int32_t* table,
+                          int32_t* refs, void* pool, int32_t* info, void* ws, size_t ws_bytes, void* stream);
+sa_status sa_pages_compact(const sa_cache4_desc* desc, int32_t max_moves, const int32_t* table, const int32_t* refs,
+                           int32_t* table_out, int32_t* refs_out, void* pool, int32_t* info, void* ws, size_t ws_bytes,
+                           void* stream);
 
 #ifdef __cplusplus
 }

@@ -20,12 +20,14 @@ SA_OP_FWD, SA_OP_BWD, SA_OP_GATED_FWD, SA_OP_GATED_BWD, SA_OP_CHECK_PERM = range
 SA_OP_GATE_PROJ_BWD, SA_OP_GATE_PROJ_BWD_SINGLE, SA_OP_DUAL_PATH_BWD, SA_OP_SAMPLE_PERM = 5, 6, 7, 8
 SA_OP_DECODE = 9
 SA_OP_BWD_ROPE = 10
+SA_OP_CACHE4_DECODE, SA_OP_PAGES_EXTEND, SA_OP_PAGES_COMPACT = 11, 12, 13
 
 EXPORTS = ("sa_status_string", "sa_workspace_bytes", "sa_check_perm", "sa_fwd", "swa_fwd",
            "gated_sa_swa_fwd", "sa_bwd", "sa_permuted_copy", "sa_gate_proj_fwd",
            "sa_gate_proj_bwd", "sa_sample_perm", "sa_dual_path_fwd", "sa_dual_path_bwd",
            "sa_rope_table", "sa_rope", "sa_fwd_rope", "sa_bwd_rope", "sa_decode_fwd", "sa_decode_fwd_varlen",
-           "sa_decode_fwd_static")
+           "sa_decode_fwd_static", "sa_cache4_pool_bytes", "sa_cache4_workspace_bytes", "sa_cache4_write", "sa_cache4_read",
+           "sa_cache4_decode_fwd", "sa_pages_fork", "sa_pages_free", "sa_pages_extend", "sa_pages_compact")
 
 
 class sa_desc(C.Structure):
@@ -34,6 +36,10 @@ class sa_desc(C.Structure):
                 ("causal_orig", C.c_int32), ("dtype", C.c_int32), ("scale", C.c_float),
                 ("perm_B", C.c_int32), ("perm_H", C.c_int32), ("gate_per_dim", C.c_int32),
                 ("gate_dtype", C.c_int32)]
+
+
+class sa_cache4_desc(C.Structure):
+    _fields_ = [(name, C.c_int32) for name in ("B", "Hq", "Hkv", "d", "page_rows", "pages", "max_pages", "layers", "dtype")] + [("scale", C.c_float)]
 
 
 class SaError(RuntimeError):
@@ -83,6 +89,25 @@ def _load():
     lib.sa_decode_fwd_static.argtypes = [dp, vp, vp, vp, C.c_int32, vp, vp, vp]
     lib.sa_decode_fwd_varlen.restype = C.c_int
     lib.sa_decode_fwd_varlen.argtypes = [dp, vp, vp, vp, ip, C.c_int32, vp, vp, vp, sz, vp]
+    cp = C.POINTER(sa_cache4_desc)
+    lib.sa_cache4_pool_bytes.restype = C.c_size_t
+    lib.sa_cache4_pool_bytes.argtypes = [cp]
+    lib.sa_cache4_workspace_bytes.restype = C.c_size_t
+    lib.sa_cache4_workspace_bytes.argtypes = [cp, C.c_int, C.c_int32]
+    lib.sa_cache4_write.restype = C.c_int
+    lib.sa_cache4_write.argtypes = [cp, vp, vp, C.c_int32] + [vp] * 5
+    lib.sa_cache4_read.restype = C.c_int
+    lib.sa_cache4_read.argtypes = [cp, vp, vp, C.c_int32] + [vp] * 5
+    lib.sa_cache4_decode_fwd.restype = C.c_int
+    lib.sa_cache4_decode_fwd.argtypes = [cp, vp, C.c_int32, vp, vp, vp, C.c_int32, vp, vp, vp, sz, vp]
+    lib.sa_pages_fork.restype = C.c_int
+    lib.sa_pages_fork.argtypes = [cp] + [vp] * 8
+    lib.sa_pages_free.restype = C.c_int
+    lib.sa_pages_free.argtypes = [cp] + [vp] * 4
+    lib.sa_pages_extend.restype = C.c_int
+    lib.sa_pages_extend.argtypes = [cp] + [vp] * 7 + [sz, vp]
+    lib.sa_pages_compact.restype = C.c_int
+    lib.sa_pages_compact.argtypes = [cp, C.c_int32] + [vp] * 7 + [sz, vp]
     lib.sa_internal_sample_perm.restype = C.c_int
     lib.sa_internal_sample_perm.argtypes = [dp, C.c_uint64, C.c_int32, ip, vp, sz, C.c_int, vp]
     lib.sa_internal_fwd_kernel.restype = C.c_char_p
@@ -226,6 +251,58 @@ def sa_decode_fwd_varlen(desc, q, K, V, lens, max_len, Y, LSE, ws):
     _check(_lib.sa_decode_fwd_varlen(C.byref(desc), _ptr(q), _ptr(K), _ptr(V), _ptr(lens), int(max_len), _ptr(Y),
                                      _ptr(LSE), _ptr(ws), (ws.numel() * ws.element_size()) if ws is not None else 0,
                                      _stream()), "sa_decode_fwd_varlen")
+
+
+def make_cache4_desc(B, Hq, Hkv, d, page_rows, pages, max_pages, layers=1, dtype=SA_BF16, scale=0.0) -> sa_cache4_desc:
+    return sa_cache4_desc(B, Hq, Hkv, d, page_rows, pages, max_pages, layers, dtype, scale)
+
+
+def sa_cache4_pool_bytes(desc: sa_cache4_desc) -> int:
+    return int(_lib.sa_cache4_pool_bytes(C.byref(desc)))
+
+
+def sa_cache4_workspace_bytes(desc: sa_cache4_desc, op: int, T: int = 1) -> int:
+    return int(_lib.sa_cache4_workspace_bytes(C.byref(desc), int(op), int(T)))
+
+
+def _ws(ws):
+    return _ptr(ws), 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def sa_cache4_write(desc, K, V, starts, counts, table, pool):
+    """K, V [B, Hkv, T, d] into the cache of one layer; starts, counts: int32 [B] or None."""
+    _check(_lib.sa_cache4_write(C.byref(desc), _ptr(K), _ptr(V), K.shape[2], _ptr(starts), _ptr(counts), _ptr(table), _ptr(pool),
+                                _stream()), "sa_cache4_write")
+
+
+def sa_cache4_read(desc, pool, table, starts, counts, K, V):
+    _check(_lib.sa_cache4_read(C.byref(desc), _ptr(pool), _ptr(table), K.shape[2], _ptr(starts), _ptr(counts), _ptr(K), _ptr(V),
+                               _stream()), "sa_cache4_read")
+
+
+def sa_cache4_decode_fwd(desc, q, pool, table, lens, max_len, Y, LSE, ws):
+    """q, Y [B, Hq, T, d]: the last T tokens of every sequence."""
+    _check(_lib.sa_cache4_decode_fwd(C.byref(desc), _ptr(q), q.shape[2], _ptr(pool), _ptr(table), _ptr(lens), int(max_len), _ptr(Y),
+                                     _ptr(LSE), *_ws(ws), _stream()), "sa_cache4_decode_fwd")
+
+
+def sa_pages_fork(desc, parents, table, lens, refs, table_out, lens_out, refs_out):
+    _check(_lib.sa_pages_fork(C.byref(desc), _ptr(parents), _ptr(table), _ptr(lens), _ptr(refs), _ptr(table_out), _ptr(lens_out),
+                              _ptr(refs_out), _stream()), "sa_pages_fork")
+
+
+def sa_pages_free(desc, keep, table, refs):
+    _check(_lib.sa_pages_free(C.byref(desc), _ptr(keep), _ptr(table), _ptr(refs), _stream()), "sa_pages_free")
+
+
+def sa_pages_extend(desc, lens, add, table, refs, pool, info, ws):
+    _check(_lib.sa_pages_extend(C.byref(desc), _ptr(lens), _ptr(add), _ptr(table), _ptr(refs), _ptr(pool), _ptr(info), *_ws(ws),
+                                _stream()), "sa_pages_extend")
+
+
+def sa_pages_compact(desc, max_moves, table, refs, table_out, refs_out, pool, info, ws):
+    _check(_lib.sa_pages_compact(C.byref(desc), int(max_moves), _ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(pool),
+                                 _ptr(info), *_ws(ws), _stream()), "sa_pages_compact")
 
 
 def swa_fwd(desc, Q, K, V, Y, LSE=None):

@@ -138,6 +138,33 @@ size_t gated_fwd_workspace(const sa_desc* c) {
   return align256((size_t)c->B * c->Hq * c->n * c->d * 2);
 }
 
+// A cache in 4 bits.  Sizes are kept where 32-bit numbers of tiles, table entries, positions and query rows hold.
+sa_status validate_cache4(const sa_cache4_desc* c) {
+  if (!c) return SA_ERR_NULL;
+  if (c->B < 1 || c->Hq < 1 || c->Hkv < 1 || c->pages < 1 || c->max_pages < 1 || c->layers < 1) return SA_ERR_SHAPE;
+  if (c->Hq % c->Hkv != 0) return SA_ERR_SHAPE;
+  if (!(c->scale == c->scale) || isinf(c->scale)) return SA_ERR_SHAPE;
+  if (!(c->d == 64 || c->d == 128)) return SA_ERR_UNSUPPORTED;
+  if (!(c->dtype == SA_BF16 || c->dtype == SA_F32)) return SA_ERR_UNSUPPORTED;
+  if (c->page_rows < 32 || c->page_rows > 1024 || (c->page_rows & (c->page_rows - 1)) != 0) return SA_ERR_UNSUPPORTED;
+  const long long tiles = c->page_rows / 32;
+  if ((long long)c->max_pages * c->page_rows > (1ll << 30) || (long long)c->B * c->max_pages > 0x7fffffffll) return SA_ERR_SHAPE;
+  if ((long long)c->pages * c->Hkv > 0x7fffffffll / tiles) return SA_ERR_SHAPE;
+  if ((long long)c->B * c->Hq > 0x7fffffffll) return SA_ERR_SHAPE;
+  if (c->Hkv > 0x7fffffffll / (tiles * 34 * c->d)) return SA_ERR_SHAPE;  // bytes of a page
+  return SA_OK;
+}
+
+bool cache4_rows_ok(const sa_cache4_desc* c, int32_t T) { return T >= 1 && (long long)c->B * c->Hq <= 0x7fffffffll / T; }
+
+// Whether [p, p + n) and [q, q + n) share a byte.
+bool overlap(const void* p, const void* q, size_t n) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+  return a < b ? b - a < n : a - b < n;
+}
+
+size_t table_bytes(const sa_cache4_desc* c) { return (size_t)c->B * c->max_pages * sizeof(int32_t); }
+
 // Scratch memory of sa_decode_fwd_static: one copy per GPU the library runs on, held until the process ends.
 // In host code the array's name is only a stand-in for the device symbol; the address a kernel may use is
 // looked up once per device (static_scratch_ptr) and kept.
@@ -636,6 +663,98 @@ sa_status sa_bwd_rope(const sa_desc* c, const void* Q, const void* K, const void
   b.Dsum_out = reinterpret_cast<float*>(base + w.off_Da);
   b.dQ = dQ; b.dK = dK; b.dV = dV; b.accumulate = 0;
   return hip_status(sa::launch_bwd_mfma_bf16(b, st));
+}
+
+size_t sa_cache4_pool_bytes(const sa_cache4_desc* c) {
+  if (validate_cache4(c) != SA_OK) return 0;
+  return (size_t)c->layers * c->pages * c->Hkv * (c->page_rows / 32) * 34 * c->d;
+}
+
+size_t sa_cache4_workspace_bytes(const sa_cache4_desc* c, int op, int32_t T) {
+  if (validate_cache4(c) != SA_OK || T < 1) return 0;
+  switch (op) {
+    case SA_OP_CACHE4_DECODE: return cache4_rows_ok(c, T) ? align256(sa::cache4_decode_workspace_bytes(c, T)) : 0;
+    case SA_OP_PAGES_EXTEND: return sa::pages_extend_workspace_bytes(c);
+    case SA_OP_PAGES_COMPACT: return sa::pages_compact_workspace_bytes(c);
+    default: return 0;
+  }
+}
+
+sa_status sa_cache4_write(const sa_cache4_desc* c, const void* K, const void* V, int32_t T, const int32_t* starts,
+                          const int32_t* counts, const int32_t* table, void* pool, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!K || !V || !table || !pool) return SA_ERR_NULL;
+  if (!cache4_rows_ok(c, T)) return SA_ERR_SHAPE;
+  if (!aligned_to(16, {K, V, pool}) || !aligned_to(4, {starts, counts, table})) return SA_ERR_UNSUPPORTED;
+  return hip_status(sa::launch_cache4_rows(c, true, const_cast<void*>(K), const_cast<void*>(V), T, starts, counts, table, pool,
+                                           (hipStream_t)stream));
+}
+
+sa_status sa_cache4_read(const sa_cache4_desc* c, const void* pool, const int32_t* table, int32_t T,
+                         const int32_t* starts, const int32_t* counts, void* K, void* V, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!K || !V || !table || !pool) return SA_ERR_NULL;
+  if (!cache4_rows_ok(c, T)) return SA_ERR_SHAPE;
+  if (!aligned_to(16, {K, V, pool}) || !aligned_to(4, {starts, counts, table})) return SA_ERR_UNSUPPORTED;
+  return hip_status(sa::launch_cache4_rows(c, false, K, V, T, starts, counts, table, const_cast<void*>(pool), (hipStream_t)stream));
+}
+
+sa_status sa_cache4_decode_fwd(const sa_cache4_desc* c, const void* q, int32_t T, const void* pool, const int32_t* table,
+                               const int32_t* lens, int32_t max_len, void* Y, float* LSE, void* ws, size_t ws_bytes, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!q || !pool || !table || !lens || !Y) return SA_ERR_NULL;
+  if (!cache4_rows_ok(c, T) || max_len < 1 || max_len > c->max_pages * c->page_rows) return SA_ERR_SHAPE;
+  if (!aligned_to(16, {q, pool, Y, ws}) || !aligned_to(4, {table, lens, LSE})) return SA_ERR_UNSUPPORTED;
+  const size_t need = sa_cache4_workspace_bytes(c, SA_OP_CACHE4_DECODE, T);
+  if (need && (!ws || ws_bytes < need)) return SA_ERR_WORKSPACE;
+  return hip_status(sa::launch_cache4_decode(c, q, T, pool, table, lens, max_len, Y, LSE, ws, (hipStream_t)stream));
+}
+
+sa_status sa_pages_fork(const sa_cache4_desc* c, const int32_t* parents, const int32_t* table, const int32_t* lens,
+                        const int32_t* refs, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!parents || !table || !lens || !refs || !table_out || !lens_out || !refs_out) return SA_ERR_NULL;
+  if (!aligned_to(4, {parents, table, lens, refs, table_out, lens_out, refs_out})) return SA_ERR_UNSUPPORTED;
+  if (overlap(table, table_out, table_bytes(c)) || overlap(lens, lens_out, (size_t)c->B * 4)) return SA_ERR_UNSUPPORTED;
+  if (refs != refs_out && overlap(refs, refs_out, (size_t)c->pages * 4)) return SA_ERR_UNSUPPORTED;
+  return hip_status(sa::launch_pages_fork(c, parents, table, lens, refs, table_out, lens_out, refs_out, (hipStream_t)stream));
+}
+
+sa_status sa_pages_free(const sa_cache4_desc* c, const int32_t* keep, int32_t* table, int32_t* refs, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!keep || !table || !refs) return SA_ERR_NULL;
+  if (!aligned_to(4, {keep, table, refs})) return SA_ERR_UNSUPPORTED;
+  return hip_status(sa::launch_pages_free(c, keep, table, refs, (hipStream_t)stream));
+}
+
+sa_status sa_pages_extend(const sa_cache4_desc* c, const int32_t* lens, const int32_t* add, int32_t* table, int32_t* refs, void* pool,
+                          int32_t* info, void* ws, size_t ws_bytes, void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!lens || !add || !table || !refs || !pool || !info) return SA_ERR_NULL;
+  if (!aligned_to(16, {pool, ws}) || !aligned_to(4, {lens, add, table, refs, info})) return SA_ERR_UNSUPPORTED;
+  if (c->B > 65535 || c->layers > 65535) return SA_ERR_UNSUPPORTED;
+  if (!ws || ws_bytes < sa::pages_extend_workspace_bytes(c)) return SA_ERR_WORKSPACE;
+  return hip_status(sa::launch_pages_extend(c, lens, add, table, refs, pool, info, ws, (hipStream_t)stream));
+}
+
+sa_status sa_pages_compact(const sa_cache4_desc* c, int32_t max_moves, const int32_t* table, const int32_t* refs,
+                           int32_t* table_out, int32_t* refs_out, void* pool, int32_t* info, void* ws, size_t ws_bytes,
+                           void* stream) {
+  sa_status s = validate_cache4(c);
+  if (s != SA_OK) return s;
+  if (!table || !refs || !table_out || !refs_out || !pool || !info) return SA_ERR_NULL;
+  if (max_moves < 0) return SA_ERR_SHAPE;
+  if (!aligned_to(16, {pool, ws}) || !aligned_to(4, {table, refs, table_out, refs_out, info})) return SA_ERR_UNSUPPORTED;
+  if (table != table_out && overlap(table, table_out, table_bytes(c))) return SA_ERR_UNSUPPORTED;
+  if (refs != refs_out && overlap(refs, refs_out, (size_t)c->pages * 4)) return SA_ERR_UNSUPPORTED;
+  if (!ws || ws_bytes < sa::pages_compact_workspace_bytes(c)) return SA_ERR_WORKSPACE;
+  return hip_status(sa::launch_pages_compact(c, max_moves, table, refs, table_out, refs_out, pool, info, ws, (hipStream_t)stream));
 }
 
 }  // extern "C"

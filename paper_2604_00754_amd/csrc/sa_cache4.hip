@@ -1,0 +1,825 @@
+// K/V caches held in 4 bits and in pages (format and tables: include/sa.h): writing rows, reading them back, attention of the
+// last T tokens of every sequence over them (the decoding of Sec. 4.2).
+//
+// Every value held is E2M1 times a power of two of at least 2^-125, an exact bf16 number: K and V enter the matrix products
+// exactly, and what rounding there is lies in q (none in bf16), in the probabilities and in the sums.
+#include <math.h>
+
+#include "sa_common.h"
+#include "sa_mfma.h"
+
+namespace sa {
+namespace {
+
+constexpr int kTile = 32;  // rows of a tile
+
+// A tile's parts, in bytes from its start, and what a lane (r, g) = (lane % 16, lane / 16) owns of it.
+template <int D>
+struct Tile {
+  static constexpr int kBytes = 34 * D;
+  static constexpr int kV = 16 * D, kKs = 32 * D, kVs = 33 * D;
+  static constexpr int E = D / 16;       // elements of a row per lane of 16
+  static constexpr int RB = D / 32;      // their bytes
+  static constexpr int LPB = 32 / E;     // lanes of a block of 32 elements
+  // row of the tile that is number j (0..7) of lane group g: 4 g .. 4 g + 3 of each half
+  static __device__ __forceinline__ int row(int g, int j) { return 16 * (j >> 2) + 4 * g + (j & 3); }
+};
+
+struct Cache {
+  unsigned char* pool;
+  const int32_t* table;
+  int B, Hkv, pages, max_pages;
+  int tiles_log2;   // tiles of a page and head
+  int capacity;     // rows of a sequence at most
+};
+
+// Number of a tile in the pool (of head hk, holding row 32 * tile of sequence b), or -1 if its page is not there.
+__device__ __forceinline__ int tile_number(const Cache& c, int b, int hk, int tile) {
+  const int page = c.table[(size_t)b * c.max_pages + (tile >> c.tiles_log2)];
+  if ((unsigned)page >= (unsigned)c.pages) return -1;
+  return ((page * c.Hkv + hk) << c.tiles_log2) + (tile & ((1 << c.tiles_log2) - 1));
+}
+
+template <int CTRL>
+__device__ __forceinline__ uint32_t max_dpp(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, true);
+  return v > o ? v : o;
+}
+// Largest over the LPB lanes of a block of 32 elements, and over the 16 lanes of a row.
+template <int LPB>
+__device__ __forceinline__ uint32_t block_max(uint32_t v) {
+  v = max_dpp<0xB1>(v);                  // quad_perm [1,0,3,2]
+  v = max_dpp<0x4E>(v);                  // quad_perm [2,3,0,1]
+  return LPB == 8 ? max_dpp<0x141>(v) : v;  // row_half_mirror
+}
+template <int LPB>
+__device__ __forceinline__ uint32_t row_max(uint32_t v) {   // of block_max's results
+  if (LPB == 4) v = max_dpp<0x141>(v);
+  return max_dpp<0x140>(v);              // row_mirror
+}
+
+template <typename T, int E>
+struct Elements;  // E neighbouring elements of a row
+
+template <int E>
+struct Elements<bf16_t, E> {
+  uint32_t w[E / 2];
+  __device__ __forceinline__ void load(const bf16_t* p) {
+    if constexpr (E == 8) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = x[i];
+    } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(p);
+      w[0] = x[0]; w[1] = x[1];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) w[i] = 0;
+  }
+  // largest magnitude as the bits of an fp32 number (an infinity or NaN is above all others)
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      const uint32_t lo = (w[i] << 16) & 0x7fffffffu, hi = w[i] & 0x7fff0000u;
+      m = m > lo ? m : lo;
+      m = m > hi ? m : hi;
+    }
+    return m;
+  }
+  __device__ __forceinline__ uint32_t codes(float scale) const {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[0]), scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[1]), scale, 1);
+    if constexpr (E == 8) {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[2]), scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, w[3]), scale, 3);
+    }
+    return c;
+  }
+};
+
+template <int E>
+struct Elements<float, E> {
+  float x[E];
+  __device__ __forceinline__ void load(const float* p) {
+#pragma unroll
+    for (int i = 0; i < E; i += 4) {
+      const f32x4 v = *reinterpret_cast<const f32x4*>(p + i);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) x[i + k] = v[k];
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = 0.f;
+  }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      const uint32_t u = __float_as_uint(x[i]) & 0x7fffffffu;
+      m = m > u ? m : u;
+    }
+    return m;
+  }
+  __device__ __forceinline__ uint32_t codes(float scale) const {
+    uint32_t c = 0;
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], scale, 0);
+    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], scale, 1);
+    if constexpr (E == 8) {
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], scale, 2);
+      c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], scale, 3);
+    }
+    return c;
+  }
+};
+
+// The scale byte of a block whose largest magnitude has the bits `top`: its exponent less 2, one more past 1.75 (7/4) of the power.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
+  const int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return (uint32_t)(e < 2 ? 2 : e);
+}
+constexpr uint32_t kNoRow = 255, kLeast = 2;
+
+struct RowsArgs {
+  Cache c;
+  const int32_t* starts;
+  const int32_t* counts;
+  void* K;
+  void* V;
+  int T, tiles;  // tiles a sequence's rows can touch
+};
+
+// What a wave of the two row kernels works on: the rows t0 + row(g, j) of one sequence and head that lie in one tile.
+struct Rows {
+  int b, hk, tile;
+  long t0;        // t of the tile's first row
+  int count;
+  bool any;
+};
+template <int WAVES>
+__device__ __forceinline__ Rows rows_of_wave(const RowsArgs& a) {
+  Rows w;
+  const long work = (long)blockIdx.x * WAVES + (threadIdx.x >> 6);
+  const int k = (int)(work % a.tiles);
+  const long bh = work / a.tiles;
+  w.any = bh < (long)a.c.B * a.c.Hkv;
+  w.hk = (int)(bh % a.c.Hkv);
+  w.b = w.any ? (int)(bh / a.c.Hkv) : 0;
+  const int start = a.starts ? a.starts[w.b] : 0;
+  w.count = a.counts ? min(max(a.counts[w.b], 0), a.T) : a.T;
+  const long tile = (long)(start >> 5) + k;
+  w.t0 = tile * kTile - start;
+  w.any = w.any && w.t0 < w.count;
+  w.tile = tile < 0 || tile * kTile >= a.c.capacity ? -1 : (int)tile;
+  return w;
+}
+
+constexpr int kRowWaves = 4;
+
+// One wave per tile that the rows touch, 8 rows a lane group, K and V of a row by the same lanes: a row that holds an infinity or
+// NaN in either is marked in both.  Bound: HBM (reads 4 d bytes a row in bf16, writes 17/16 d).
+template <typename T, int D>
+__global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a) {
+  using L = Tile<D>;
+  constexpr int E = L::E;
+  const Rows w = rows_of_wave<kRowWaves>(a);
+  if (!w.any || w.tile < 0) return;
+  const int number = tile_number(a.c, w.b, w.hk, w.tile);
+  if (number < 0) return;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
+  unsigned char* base = a.c.pool + (size_t)number * L::kBytes;
+  const size_t src = ((size_t)w.b * a.c.Hkv + w.hk) * a.T;
+  Elements<T, E> k[8], v[8];
+  bool in[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const long t = w.t0 + L::row(g, j);
+    in[j] = t >= 0 && t < w.count;
+    if (in[j]) {
+      const size_t at = (src + (size_t)t) * D + r * E;
+      k[j].load(reinterpret_cast<const T*>(a.K) + at);
+      v[j].load(reinterpret_cast<const T*>(a.V) + at);
+    } else {
+      k[j].clear();
+      v[j].clear();
+    }
+  }
+  uint32_t kc[8], vc[8], ks[8], vs[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const uint32_t kt = block_max<L::LPB>(k[j].top()), vt = block_max<L::LPB>(v[j].top());
+    const bool bad = row_max<L::LPB>(kt > vt ? kt : vt) >= 0x7f800000u;
+    ks[j] = scale_byte(kt);
+    vs[j] = scale_byte(vt);
+    kc[j] = k[j].codes(__uint_as_float(ks[j] << 23));
+    vc[j] = v[j].codes(__uint_as_float(vs[j] << 23));
+    if (bad) { kc[j] = 0; vc[j] = 0; ks[j] = kNoRow; vs[j] = kLeast; }
+  }
+  bool all = true;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) all = all && in[j];
+  // K codes: rows as they are; V codes: the 8 rows of a lane group side by side
+  unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (in[j]) {
+      unsigned char* kp = base + L::row(g, j) * (D / 2) + r * L::RB;
+      if constexpr (L::RB == 4) *reinterpret_cast<uint32_t*>(kp) = kc[j];
+      else *reinterpret_cast<uint16_t*>(kp) = (uint16_t)kc[j];
+    }
+  if (all) {
+    if constexpr (L::RB == 4) {
+      reinterpret_cast<u32x4*>(vp)[0] = u32x4{vc[0], vc[1], vc[2], vc[3]};
+      reinterpret_cast<u32x4*>(vp)[1] = u32x4{vc[4], vc[5], vc[6], vc[7]};
+    } else {
+      *reinterpret_cast<u32x4*>(vp) = u32x4{(vc[0] & 0xffffu) | (vc[1] << 16), (vc[2] & 0xffffu) | (vc[3] << 16),
+                                            (vc[4] & 0xffffu) | (vc[5] << 16), (vc[6] & 0xffffu) | (vc[7] << 16)};
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (in[j]) {
+        if constexpr (L::RB == 4) reinterpret_cast<uint32_t*>(vp)[j] = vc[j];
+        else reinterpret_cast<uint16_t*>(vp)[j] = (uint16_t)vc[j];
+      }
+  }
+  if (r % L::LPB == 0) {  // the first lane of a block keeps its scales
+    const int c = r / L::LPB;
+    unsigned char* kq = base + L::kKs + (c * 16 + 4 * g) * 2;
+    unsigned char* vq = base + L::kVs + (c * 4 + g) * 8;
+    if (all) {
+      *reinterpret_cast<u32x2*>(kq) = u32x2{ks[0] | ks[4] << 8 | ks[1] << 16 | ks[5] << 24, ks[2] | ks[6] << 8 | ks[3] << 16 | ks[7] << 24};
+      *reinterpret_cast<u32x2*>(vq) = u32x2{vs[0] | vs[1] << 8 | vs[2] << 16 | vs[3] << 24, vs[4] | vs[5] << 8 | vs[6] << 16 | vs[7] << 24};
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (in[j]) {
+          kq[2 * (j & 3) + (j >> 2)] = (unsigned char)ks[j];
+          vq[j] = (unsigned char)vs[j];
+        }
+    }
+  }
+}
+
+// E elements from their codes (low bytes of c), times the scale
+template <typename T, int E>
+__device__ __forceinline__ void store_values(T* p, uint32_t c, float scale, bool nan, bool there);
+template <>
+__device__ __forceinline__ void store_values<bf16_t, 8>(bf16_t* p, uint32_t c, float s, bool nan, bool there) {
+  u32x4 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+  o[2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 2));
+  o[3] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 3));
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = there ? (nan ? 0x7fc07fc0u : o[i]) : 0u;
+  *reinterpret_cast<u32x4*>(p) = o;
+}
+template <>
+__device__ __forceinline__ void store_values<bf16_t, 4>(bf16_t* p, uint32_t c, float s, bool nan, bool there) {
+  u32x2 o;
+  o[0] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 0));
+  o[1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, s, 1));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) o[i] = there ? (nan ? 0x7fc07fc0u : o[i]) : 0u;
+  *reinterpret_cast<u32x2*>(p) = o;
+}
+__device__ __forceinline__ void store4(float* p, f32x2 a, f32x2 b, bool nan, bool there) {
+  const float q = __uint_as_float(0x7fc00000u);
+  f32x4 o = {a[0], a[1], b[0], b[1]};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) o[i] = there ? (nan ? q : o[i]) : 0.f;
+  *reinterpret_cast<f32x4*>(p) = o;
+}
+template <>
+__device__ __forceinline__ void store_values<float, 4>(float* p, uint32_t c, float s, bool nan, bool there) {
+  store4(p, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 1), nan, there);
+}
+template <>
+__device__ __forceinline__ void store_values<float, 8>(float* p, uint32_t c, float s, bool nan, bool there) {
+  store_values<float, 4>(p, c, s, nan, there);
+  store4(p + 4, __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, s, 3), nan, there);
+}
+
+// The reverse, lane for lane.  Bound: HBM (writes).
+template <typename T, int D>
+__global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a) {
+  using L = Tile<D>;
+  const Rows w = rows_of_wave<kRowWaves>(a);
+  if (!w.any) return;
+  const int number = w.tile < 0 ? -1 : tile_number(a.c, w.b, w.hk, w.tile);
+  const bool there = number >= 0;
+  const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, c = r / L::LPB;
+  const unsigned char* base = a.c.pool + (size_t)(there ? number : 0) * L::kBytes;
+  uint32_t kc[8] = {}, vc[8] = {};
+  u32x2 ks = {}, vs = {};
+  if (there) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const unsigned char* kp = base + L::row(g, j) * (D / 2) + r * L::RB;
+      if constexpr (L::RB == 4) kc[j] = *reinterpret_cast<const uint32_t*>(kp);
+      else kc[j] = *reinterpret_cast<const uint16_t*>(kp);
+    }
+    const unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
+    const u32x4 x = reinterpret_cast<const u32x4*>(vp)[0];
+    if constexpr (L::RB == 4) {
+      const u32x4 y = reinterpret_cast<const u32x4*>(vp)[1];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) { vc[j] = x[j]; vc[4 + j] = y[j]; }
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vc[j] = (x[j / 2] >> (16 * (j & 1))) & 0xffffu;
+    }
+    ks = *reinterpret_cast<const u32x2*>(base + L::kKs + (c * 16 + 4 * g) * 2);
+    vs = *reinterpret_cast<const u32x2*>(base + L::kVs + (c * 4 + g) * 8);
+  }
+  const size_t dst = ((size_t)w.b * a.c.Hkv + w.hk) * a.T;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const long t = w.t0 + L::row(g, j);
+    const uint32_t kb = (ks[(j & 3) / 2] >> (16 * (j & 1) + 8 * (j >> 2))) & 0xffu, vb = (vs[j / 4] >> (8 * (j & 3))) & 0xffu;
+    if (t >= 0 && t < w.count) {
+      const size_t at = (dst + (size_t)t) * D + r * L::E;
+      const bool nan = kb == kNoRow;
+      store_values<T, L::E>(reinterpret_cast<T*>(a.K) + at, kc[j], __uint_as_float(kb << 23), nan, there);
+      store_values<T, L::E>(reinterpret_cast<T*>(a.V) + at, vc[j], __uint_as_float(vb << 23), nan, there);
+    }
+  }
+}
+
+// ---- attention ----------------------------------------------------------------------------------------------------------------
+//
+// The g query heads of a KV head and the T tokens are g T query rows that read the same cache: rows c = h T + t, as they lie in
+// memory.  A wave takes NT blocks of 16 of them and a tile of 32 cached rows at a time:
+//   S^T (16 cached rows x 16 query rows, twice) = K Q^T, lane (r, g) holding cached row r, elements D/4 g .. of it as they lie in
+//   the tile (which elements a lane group takes in a step is free as long as Q's operand agrees); the result leaves lane (c, g)
+//   with query row c and cached rows 4 g + i of each half;
+//   O^T (16 elements x 16 query rows, D/16 times) += V^T P^T, where those scores are the operand P^T as they stand and lane (r, g) holds
+//   elements E r .. E r + E - 1 of the same 8 cached rows: the order in which V lies in the tile.
+// 4-bit codes become bf16 pairs by one conversion each, which multiplies by the power of two as well; V's pairs are re-paired
+// over two rows by byte permutes.  The maximum of a query row is raised only where a score passes it by more than 2^8: the
+// sums stay far inside fp32's range, and the usual tile needs no exchange between lanes and no product with a correction.
+struct AttnArgs {
+  Cache c;
+  const void* q;
+  void* Y;
+  float* LSE;
+  float* part;  // [B*Hq*T][splits][D + 2]: weighted V sum, maximum (log2 domain), sum
+  const int32_t* lens;
+  int T, rows, row_blocks, max_len, chunk, splits;
+  float scale_log2e;
+};
+
+__device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
+
+// x as PARTS bf16 numbers whose sum is x to 8, 17 or 24 bits, in the words w[part] of two elements
+template <int PARTS>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t* w) {
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    w[p] = pack_bf16(x, y);
+    if (p + 1 < PARTS) {
+      x -= bf16lo(w[p]);
+      y -= bf16hi(w[p]);
+    }
+  }
+}
+
+__device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+constexpr int kAttnWaves = 4;
+
+template <int D>
+struct TileRegs {
+  uint32_t k[2][D / 32];  // [half][word]: 8 elements a word
+  uint32_t v[D / 16];     // D = 128: a word per row j; D = 64: rows 2j, 2j + 1 share one
+  uint32_t ks;            // scale bytes of the halves
+  u32x2 vs;               // of rows j
+  __device__ __forceinline__ void load(const unsigned char* base, int r, int g) {
+    using L = Tile<D>;
+    const unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
+    if constexpr (D == 128) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(base + (16 * h + r) * 64 + 16 * g);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) k[h][i] = x[i];
+      }
+      const u32x4 a = reinterpret_cast<const u32x4*>(vp)[0], b = reinterpret_cast<const u32x4*>(vp)[1];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+      ks = *reinterpret_cast<const uint16_t*>(base + L::kKs + (g * 16 + r) * 2);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(base + (16 * h + r) * 32 + 8 * g);
+        k[h][0] = x[0]; k[h][1] = x[1];
+      }
+      const u32x4 a = *reinterpret_cast<const u32x4*>(vp);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[i] = a[i];
+      ks = *reinterpret_cast<const uint16_t*>(base + L::kKs + ((g >> 1) * 16 + r) * 2);
+    }
+    vs = *reinterpret_cast<const u32x2*>(base + L::kVs + ((r / L::LPB) * 4 + g) * 8);
+  }
+};
+
+template <int SEL>
+__device__ __forceinline__ uint32_t two_values(uint32_t codes, float scale) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+}
+__device__ __forceinline__ bf16x8 eight_values(uint32_t codes, float scale) {
+  const u32x4 w = {two_values<0>(codes, scale), two_values<1>(codes, scale), two_values<2>(codes, scale), two_values<3>(codes, scale)};
+  return __builtin_bit_cast(bf16x8, w);
+}
+
+template <typename T>
+__device__ __forceinline__ void load_q8(const T* p, float (&x)[8]);
+template <>
+__device__ __forceinline__ void load_q8<bf16_t>(const bf16_t* p, float (&x)[8]) {
+  const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[2 * i] = bf16lo(v[i]); x[2 * i + 1] = bf16hi(v[i]); }
+}
+template <>
+__device__ __forceinline__ void load_q8<float>(const float* p, float (&x)[8]) {
+  const f32x4 a = reinterpret_cast<const f32x4*>(p)[0], b = reinterpret_cast<const f32x4*>(p)[1];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) { x[i] = a[i]; x[4 + i] = b[i]; }
+}
+
+__device__ __forceinline__ void store_y(bf16_t* p, float v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
+__device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
+
+template <typename T, int D, int NT>
+__global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a) {
+  using L = Tile<D>;
+  constexpr int QP = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of q
+  constexpr int PP = sizeof(T) == 2 ? 2 : 3;   // and of a probability
+  constexpr int KS = D / 32;                   // steps of the score product
+  constexpr int DB = D / 16;                   // blocks of 16 elements
+  constexpr int LD = D + 4;                    // floats between rows of the merge area
+  __shared__ __align__(16) float lds_o[kAttnWaves][16][LD];
+  __shared__ float lds_ml[kAttnWaves][16][2];
+
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int split = (int)(blockIdx.x % (unsigned)a.splits);
+  const unsigned rest = blockIdx.x / (unsigned)a.splits;
+  const int rb = (int)(rest % (unsigned)a.row_blocks);
+  const int bh = (int)(rest / (unsigned)a.row_blocks);
+  const int hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
+  const int row0 = rb * 16 * NT;
+  const int len = min(max(a.lens[b], 0), a.max_len);
+
+  // the last position each of the lane's query rows sees (-1 or less: none), and their largest and smallest over the block
+  int last[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int c = row0 + 16 * n + r;
+    last[n] = c < a.rows ? len - a.T + c % a.T : -1;
+  }
+  const int c1 = min(row0 + 16 * NT, a.rows) - 1;
+  const bool one_head = row0 / a.T == c1 / a.T;
+  const int most = len - a.T + (one_head ? c1 % a.T : a.T - 1), least = len - a.T + (one_head ? row0 % a.T : 0);
+
+  const T* qrows = reinterpret_cast<const T*>(a.q) + (size_t)bh * a.rows * D;
+  bf16x8 qf[NT][KS][QP];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int c = min(row0 + 16 * n + r, a.rows - 1);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      float x[8];
+      load_q8<T>(qrows + (size_t)c * D + (D / 4) * g + 8 * s, x);
+      u32x4 w[QP];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p[QP];
+        split_pair<QP>(x[2 * i], x[2 * i + 1], p);
+#pragma unroll
+        for (int k = 0; k < QP; ++k) w[k][i] = p[k];
+      }
+#pragma unroll
+      for (int k = 0; k < QP; ++k) qf[n][s][k] = __builtin_bit_cast(bf16x8, w[k]);
+    }
+  }
+
+  f32x4 o[NT][DB];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+#pragma unroll
+    for (int d = 0; d < DB; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    m[n] = -INFINITY;
+    l[n] = 0.f;
+  }
+
+  const int t0 = split * a.chunk, t1 = min(t0 + a.chunk, most < 0 ? 0 : most / kTile + 1);
+  for (int first = t0 + wave; first < t1; first += 64 * kAttnWaves) {
+    // the page table's entries of the wave's next 64 tiles, one a lane
+    const int mine = first + kAttnWaves * lane;
+    const int numbers = mine < t1 ? tile_number(a.c, b, hk, mine) : -1;
+    const int turns = min(64, (t1 - first + kAttnWaves - 1) / kAttnWaves);
+    for (int i = 0; i < turns; ++i) {
+      const int number = __builtin_amdgcn_readlane(numbers, i);
+      if (number < 0) continue;
+      const int tile = first + kAttnWaves * i;
+      TileRegs<D> x;
+      x.load(a.c.pool + (size_t)number * L::kBytes, r, g);
+
+      const bool partly = tile * kTile + kTile - 1 > least;  // some query row does not see all of it
+      // scores
+      f32x4 sc[NT][2];
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const float s = __uint_as_float(((x.ks >> (8 * h)) & 0xffu) << 23);
+        const float scale = ((x.ks >> (8 * h)) & 0xffu) == kNoRow ? __uint_as_float(0x7fc00000u) : s;
+        bf16x8 kf[KS];
+#pragma unroll
+        for (int st = 0; st < KS; ++st) kf[st] = eight_values(x.k[h][st], scale);
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = QP - 1; k >= 0; --k)
+#pragma unroll
+            for (int st = 0; st < KS; ++st) acc = mfma16(kf[st], qf[n][st][k], acc);
+          sc[n][h] = acc;
+        }
+      }
+      bf16x8 p[NT][PP];
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            float s = sc[n][h][e] * a.scale_log2e;
+            if (partly && tile * kTile + 16 * h + 4 * g + e > last[n]) s = -INFINITY;
+            sc[n][h][e] = s;
+            top = fmaxf(top, s);
+          }
+        if (__any(top > m[n] + 8.f)) {   // (m = -inf at first)
+          float mn = fmaxf(top, __shfl_xor(top, 16));
+          mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
+          const float corr = exp2_above(m[n], mn);
+          l[n] *= corr;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[n][d] *= corr;
+          m[n] = mn;
+        }
+        const float ref = m[n] == -INFINITY ? 0.f : m[n];
+        u32x4 w[PP];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int e = 0; e < 4; e += 2) {
+            const float p0 = exp2f(sc[n][h][e] - ref), p1 = exp2f(sc[n][h][e + 1] - ref);
+            l[n] += p0 + p1;
+            uint32_t parts[PP];
+            split_pair<PP>(p0, p1, parts);
+#pragma unroll
+            for (int k = 0; k < PP; ++k) w[k][2 * h + e / 2] = parts[k];
+          }
+#pragma unroll
+        for (int k = 0; k < PP; ++k) p[n][k] = __builtin_bit_cast(bf16x8, w[k]);
+      }
+      // V: words of rows j -> operands of blocks 2q, 2q + 1, rows in pairs
+      float vsc[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        uint32_t byte = (x.vs[j / 4] >> (8 * (j & 3))) & 0xffu;
+        if (partly && tile * kTile + L::row(g, j) >= len) byte = 0;  // never written: whatever lies there is kept finite
+        vsc[j] = __uint_as_float(byte << 23);
+      }
+#pragma unroll
+      for (int q = 0; q < DB / 2; ++q) {
+        uint32_t pr[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (D == 128) {
+            pr[j] = q == 0 ? two_values<0>(x.v[j], vsc[j]) : q == 1 ? two_values<1>(x.v[j], vsc[j]) : q == 2 ? two_values<2>(x.v[j], vsc[j]) : two_values<3>(x.v[j], vsc[j]);
+          } else {
+            pr[j] = (j & 1) ? (q ? two_values<3>(x.v[j / 2], vsc[j]) : two_values<2>(x.v[j / 2], vsc[j]))
+                            : (q ? two_values<1>(x.v[j / 2], vsc[j]) : two_values<0>(x.v[j / 2], vsc[j]));
+          }
+        }
+        u32x4 lo, hi;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
+          hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
+        }
+        const bf16x8 flo = __builtin_bit_cast(bf16x8, lo), fhi = __builtin_bit_cast(bf16x8, hi);
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int k = PP - 1; k >= 0; --k) {
+            o[n][2 * q] = mfma16(flo, p[n][k], o[n][2 * q]);
+            o[n][2 * q + 1] = mfma16(fhi, p[n][k], o[n][2 * q + 1]);
+          }
+      }
+    }
+  }
+
+  // the waves' results, 16 query rows at a time
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    float ls = l[n];
+    ls += __shfl_xor(ls, 16);
+    ls += __shfl_xor(ls, 32);
+    if (n > 0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int d = 0; d < DB; ++d) lds_o[wave][r][DB * (4 * g + i) + d] = o[n][d][i];
+    if (g == 0) {
+      lds_ml[wave][r][0] = m[n];
+      lds_ml[wave][r][1] = ls;
+    }
+    __syncthreads();
+    for (int idx = threadIdx.x; idx < 16 * D; idx += kAttnWaves * 64) {
+      const int c = idx / D, e = idx % D;
+      const int row = row0 + 16 * n + c;
+      if (row >= a.rows) continue;
+      float M = lds_ml[0][c][0];
+#pragma unroll
+      for (int w = 1; w < kAttnWaves; ++w) M = fmaxf(M, lds_ml[w][c][0]);
+      float v = 0.f, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < kAttnWaves; ++w) {
+        const float f = exp2_above(lds_ml[w][c][0], M);
+        v = fmaf(f, lds_o[w][c][e], v);
+        sum = fmaf(f, lds_ml[w][c][1], sum);
+      }
+      const size_t out = (size_t)bh * a.rows + row;
+      if (a.splits == 1) {
+        store_y(reinterpret_cast<T*>(a.Y) + out * D + e, sum == 0.f ? 0.f : v / sum);
+        if (e == 0 && a.LSE) a.LSE[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+      } else {
+        float* to = a.part + (out * a.splits + split) * (D + 2);
+        to[e] = v;
+        if (e == 0) {
+          to[D] = M;
+          to[D + 1] = sum;
+        }
+      }
+    }
+  }
+}
+
+constexpr int kMergeWaves = 8;
+
+// One workgroup per query row joins the splits' results: each wave runs over its own with a running maximum.
+template <typename T, int D>
+__global__ __launch_bounds__(kMergeWaves * 64) void cache4_merge_kernel(const float* __restrict__ part, T* __restrict__ Y,
+                                                                         float* __restrict__ LSE, int splits) {
+  constexpr int EPL = D / 64, UM = 4;
+  __shared__ float lds_m[kMergeWaves], lds_l[kMergeWaves], lds_o[kMergeWaves][D];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float* P = part + (size_t)blockIdx.x * splits * (D + 2);
+  float m = -INFINITY, l = 0.f, o[EPL] = {};
+  for (int s0 = wave; s0 < splits; s0 += kMergeWaves * UM) {
+    float mx[UM], lx[UM], x[UM][EPL], mn = m;
+#pragma unroll
+    for (int u = 0; u < UM; ++u) {
+      const int s = s0 + u * kMergeWaves;
+      const float* row = P + (size_t)min(s, splits - 1) * (D + 2);
+      mx[u] = s < splits ? row[D] : -INFINITY;
+      lx[u] = s < splits ? row[D + 1] : 0.f;
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) x[u][i] = s < splits ? row[lane + 64 * i] : 0.f;
+      mn = fmaxf(mn, mx[u]);
+    }
+    const float corr = exp2_above(m, mn);
+    l *= corr;
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) o[i] *= corr;
+#pragma unroll
+    for (int u = 0; u < UM; ++u) {
+      const float f = exp2_above(mx[u], mn);
+      l = fmaf(f, lx[u], l);
+#pragma unroll
+      for (int i = 0; i < EPL; ++i) o[i] = fmaf(f, x[u][i], o[i]);
+    }
+    m = mn;
+  }
+#pragma unroll
+  for (int i = 0; i < EPL; ++i) lds_o[wave][lane + 64 * i] = o[i];
+  if (lane == 0) {
+    lds_m[wave] = m;
+    lds_l[wave] = l;
+  }
+  __syncthreads();
+  if (threadIdx.x < D) {
+    const int e = threadIdx.x;
+    float M = lds_m[0], sum = 0.f, v = 0.f;
+#pragma unroll
+    for (int w = 1; w < kMergeWaves; ++w) M = fmaxf(M, lds_m[w]);
+#pragma unroll
+    for (int w = 0; w < kMergeWaves; ++w) {
+      const float f = exp2_above(lds_m[w], M);
+      sum = fmaf(f, lds_l[w], sum);
+      v = fmaf(f, lds_o[w][e], v);
+    }
+    store_y(Y + (size_t)blockIdx.x * D + e, sum == 0.f ? 0.f : v / sum);
+    if (e == 0 && LSE) LSE[blockIdx.x] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  }
+}
+
+int log2_of(int v) { int k = 0; while ((1 << k) < v) ++k; return k; }
+
+Cache cache_of(const sa_cache4_desc* c, void* pool, const int32_t* table) {
+  Cache k;
+  k.pool = reinterpret_cast<unsigned char*>(pool);
+  k.table = table;
+  k.B = c->B; k.Hkv = c->Hkv; k.pages = c->pages; k.max_pages = c->max_pages;
+  k.tiles_log2 = log2_of(c->page_rows / kTile);
+  k.capacity = c->max_pages * c->page_rows;
+  return k;
+}
+
+int row_tiles(long rows) { return rows > 32 ? 4 : rows > 16 ? 2 : 1; }
+
+// Workgroups wanted; a cache of `tiles` tiles read by `groups` workgroups otherwise is cut into that many pieces.
+constexpr long kWanted = 512;
+long splits_for(long groups, long tiles) {
+  const long want = (kWanted + groups - 1) / groups, most = (tiles + kAttnWaves - 1) / kAttnWaves;
+  return want < most ? want : most;
+}
+
+long groups_of(const sa_cache4_desc* c, int T) {
+  const long rows = (long)(c->Hq / c->Hkv) * T, nt = row_tiles(rows);
+  return (long)c->B * c->Hkv * ((rows + 16 * nt - 1) / (16 * nt));
+}
+
+template <typename T, int D>
+hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, hipStream_t st) {
+  const int nt = row_tiles(a.rows);
+  a.row_blocks = (a.rows + 16 * nt - 1) / (16 * nt);
+  const long blocks = (long)c->B * c->Hkv * a.row_blocks * a.splits;
+  if (blocks > 0x7fffffffL) return hipErrorNotSupported;
+  const unsigned grid = (unsigned)blocks;
+  if (nt == 1) cache4_attn_kernel<T, D, 1><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  else if (nt == 2) cache4_attn_kernel<T, D, 2><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  else cache4_attn_kernel<T, D, 4><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.splits == 1) return e;
+  cache4_merge_kernel<T, D><<<(unsigned)(c->B * c->Hq * a.T), kMergeWaves * 64, 0, st>>>(a.part, reinterpret_cast<T*>(a.Y), a.LSE, a.splits);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void* V, int T, const int32_t* starts,
+                              const int32_t* counts, const int32_t* table, void* pool, hipStream_t st) {
+  RowsArgs a;
+  a.c = cache_of(c, pool, table);
+  a.starts = starts; a.counts = counts; a.K = K; a.V = V; a.T = T;
+  a.tiles = (int)(((long)T + 62) / kTile);  // the first and the last may be begun
+  const long blocks = ((long)c->B * c->Hkv * a.tiles + kRowWaves - 1) / kRowWaves;
+  if (blocks > 0x7fffffffL) return hipErrorNotSupported;
+  const unsigned grid = (unsigned)blocks;
+  const dim3 block(kRowWaves * 64);
+  const bool bf16 = c->dtype == SA_BF16;
+  if (write) {
+    if (bf16 && c->d == 128) cache4_write_kernel<bf16_t, 128><<<grid, block, 0, st>>>(a);
+    else if (bf16) cache4_write_kernel<bf16_t, 64><<<grid, block, 0, st>>>(a);
+    else if (c->d == 128) cache4_write_kernel<float, 128><<<grid, block, 0, st>>>(a);
+    else cache4_write_kernel<float, 64><<<grid, block, 0, st>>>(a);
+  } else {
+    if (bf16 && c->d == 128) cache4_read_kernel<bf16_t, 128><<<grid, block, 0, st>>>(a);
+    else if (bf16) cache4_read_kernel<bf16_t, 64><<<grid, block, 0, st>>>(a);
+    else if (c->d == 128) cache4_read_kernel<float, 128><<<grid, block, 0, st>>>(a);
+    else cache4_read_kernel<float, 64><<<grid, block, 0, st>>>(a);
+  }
+  return hipGetLastError();
+}
+
+size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T) {
+  const long tiles = ((long)c->max_pages * c->page_rows) / kTile;
+  const long splits = splits_for(groups_of(c, T), tiles);
+  return splits <= 1 ? 0 : (size_t)c->B * c->Hq * T * (size_t)splits * (c->d + 2) * sizeof(float);
+}
+
+hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, const void* pool, const int32_t* table,
+                                const int32_t* lens, int max_len, void* Y, float* LSE, void* ws, hipStream_t st) {
+  AttnArgs a;
+  a.c = cache_of(c, const_cast<void*>(pool), table);
+  a.q = q; a.Y = Y; a.LSE = LSE; a.part = reinterpret_cast<float*>(ws); a.lens = lens;
+  a.T = T; a.rows = (c->Hq / c->Hkv) * T; a.max_len = max_len;
+  const long tiles = ((long)max_len + kTile - 1) / kTile;
+  const long splits = splits_for(groups_of(c, T), tiles);
+  a.chunk = (int)((tiles + splits - 1) / splits);
+  a.splits = (int)((tiles + a.chunk - 1) / a.chunk);
+  a.scale_log2e = (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->d)) * kLog2e;
+  if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, st) : launch_attn<bf16_t, 64>(c, a, st);
+  return c->d == 128 ? launch_attn<float, 128>(c, a, st) : launch_attn<float, 64>(c, a, st);
+}
+
+}  // namespace sa

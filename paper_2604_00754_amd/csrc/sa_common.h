@@ -110,6 +110,22 @@ struct Decode {
 size_t decode_workspace_bytes(int B, int Hq, int Hkv, int n, int d);
 hipError_t launch_decode(const Decode& d, hipStream_t st);
 
+// sa_cache4.hip, sa_pages.hip: caches in 4 bits and in pages.  K, V of the rows: written, or (write = false) read back into
+hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void* V, int T, const int32_t* starts,
+                              const int32_t* counts, const int32_t* table, void* pool, hipStream_t st);
+size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T);
+hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, const void* pool, const int32_t* table,
+                                const int32_t* lens, int max_len, void* Y, float* LSE, void* ws, hipStream_t st);
+size_t pages_extend_workspace_bytes(const sa_cache4_desc* c);
+size_t pages_compact_workspace_bytes(const sa_cache4_desc* c);
+hipError_t launch_pages_fork(const sa_cache4_desc* c, const int32_t* parents, const int32_t* table, const int32_t* lens, const int32_t* refs,
+                             int32_t* table_out, int32_t* lens_out, int32_t* refs_out, hipStream_t st);
+hipError_t launch_pages_free(const sa_cache4_desc* c, const int32_t* keep, int32_t* table, int32_t* refs, hipStream_t st);
+hipError_t launch_pages_extend(const sa_cache4_desc* c, const int32_t* lens, const int32_t* add, int32_t* table, int32_t* refs, void* pool,
+                               int32_t* info, void* ws, hipStream_t st);
+hipError_t launch_pages_compact(const sa_cache4_desc* c, int max_moves, const int32_t* table, const int32_t* refs, int32_t* table_out,
+                                int32_t* refs_out, void* pool, int32_t* info, void* ws, hipStream_t st);
+
 // helpers in sa_misc.hip
 hipError_t launch_check_perm(const int32_t* perm, int slices, int n, int* seen, int* flag,
                              hipStream_t st);

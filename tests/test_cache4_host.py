@@ -1,0 +1,163 @@
+"""Caches held in 4 bits, without a GPU: the oracle against facts about the format, and the refusals of the entry points."""
+import ctypes as C
+
+import numpy as np
+import pytest
+
+from oracle import cache4 as orc
+from paper_2604_00754_amd import binding as sa
+
+FAKE = C.c_void_p(4096)  # never dereferenced: every call below fails validation first
+FAR = C.c_void_p(1 << 40)
+
+
+# ---- the oracle ---------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("e", [-125, -20, 0, 5, 120])
+def test_what_the_format_holds_stays_as_it_is(e):
+    x = np.array([s * m * 2.0 ** e for s in (1, -1) for m in orc.MAGNITUDES] * 2)
+    (codes, byte), _ = orc.quantise_row(x, x)
+    assert byte == [e + 127] and [orc.value(c, byte[0]) for c in codes] == list(x)
+
+
+def test_ties_go_to_the_even_code_and_the_scale_turns_at_seven():
+    codes = [orc.element_code(v, 0) for v in (0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 7.5)]
+    assert codes == [0, 2, 2, 4, 4, 6, 6, 7]
+    assert orc.block_exponent(7.0) == 0 and orc.block_exponent(np.nextafter(7.0, 8)) == 1
+    assert orc.block_exponent(4.0) == 0 and orc.block_exponent(np.nextafter(4.0, 0)) == 0  # 3.99.. / 2^-1 > 7
+    assert orc.block_exponent(3.5) == -1 and orc.block_exponent(2.0 ** -149) == -125 and orc.block_exponent(0.0) == -125
+
+
+def test_normal_rows_are_held_as_well_as_the_better_of_two_powers_holds_them():
+    """Relative error 0.112 of N(0,1) rows, within 1 % of choosing the power of every block by its error."""
+    x = np.random.default_rng(0).standard_normal((300, 32))
+    err = best = 0.0
+    for row in x:
+        by = {}
+        e = orc.block_exponent(np.abs(row).max())
+        for k in (e - 1, e, e + 1):
+            by[k] = sum((orc.value(orc.element_code(v, k), k + 127) - v) ** 2 for v in row)
+        err += by[e]
+        best += min(by.values())
+    assert err <= 1.02 * best and np.sqrt(err / (x ** 2).sum()) < 0.115
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_byte_of_a_tile_has_one_place(d):
+    c = orc.Cache(1, d, 32, 1)
+    places = np.concatenate([np.concatenate(c._places(r)) for r in range(32)])
+    assert sorted(places) == list(range(34 * d))
+
+
+# ---- refusals -----------------------------------------------------------------------------------------------------------------
+
+
+def desc(**kw):
+    a = dict(B=2, Hq=8, Hkv=2, d=128, page_rows=64, pages=40, max_pages=16, layers=3, dtype=sa.SA_BF16, scale=0.0)
+    a.update(kw)
+    return sa.make_cache4_desc(**a)
+
+
+def calls(d, **kw):
+    """Every entry point with good arguments but those in kw, by name -> status"""
+    a = dict(K=FAKE, V=FAKE, T=5, starts=FAKE, counts=FAKE, table=FAKE, pool=FAKE, q=FAKE, lens=FAKE, max_len=1000, Y=FAKE, LSE=FAKE, ws=FAKE,
+             ws_bytes=1 << 40, parents=FAKE, refs=FAKE, table_out=FAR, lens_out=FAR, refs_out=FAKE, keep=FAKE, add=FAKE, info=FAKE, max_moves=9)
+    a.update(kw)
+    p = C.byref(d) if d is not None else None
+    lib = sa.raw()
+    order = {"sa_cache4_write": "K V T starts counts table pool", "sa_cache4_read": "pool table T starts counts K V",
+             "sa_cache4_decode_fwd": "q T pool table lens max_len Y LSE ws ws_bytes",
+             "sa_pages_fork": "parents table lens refs table_out lens_out refs_out", "sa_pages_free": "keep table refs",
+             "sa_pages_extend": "lens add table refs pool info ws ws_bytes",
+             "sa_pages_compact": "max_moves table refs table_out refs_out pool info ws ws_bytes"}
+    out = {}
+    for name, args in order.items():
+        args = args.split()
+        if not kw or any(k in args for k in kw):
+            out[name] = getattr(lib, name)(p, *[a[k] for k in args], None)
+    return out
+
+
+def test_null_descriptor():
+    assert set(calls(None).values()) == {sa.SA_ERR_NULL}
+
+
+@pytest.mark.parametrize("field,value,status", [
+    ("B", 0, sa.SA_ERR_SHAPE), ("Hq", 0, sa.SA_ERR_SHAPE), ("Hkv", 3, sa.SA_ERR_SHAPE), ("pages", 0, sa.SA_ERR_SHAPE),
+    ("max_pages", 0, sa.SA_ERR_SHAPE), ("layers", 0, sa.SA_ERR_SHAPE), ("layers", -1, sa.SA_ERR_SHAPE), ("scale", float("inf"), sa.SA_ERR_SHAPE),
+    ("scale", float("nan"), sa.SA_ERR_SHAPE), ("d", 96, sa.SA_ERR_UNSUPPORTED), ("dtype", 2, sa.SA_ERR_UNSUPPORTED),
+    ("page_rows", 16, sa.SA_ERR_UNSUPPORTED), ("page_rows", 96, sa.SA_ERR_UNSUPPORTED), ("page_rows", 2048, sa.SA_ERR_UNSUPPORTED),
+    ("page_rows", 0, sa.SA_ERR_UNSUPPORTED), ("page_rows", -64, sa.SA_ERR_UNSUPPORTED),
+    ("max_pages", (1 << 30) // 64 + 1, sa.SA_ERR_SHAPE), ("B", 1 << 27, sa.SA_ERR_SHAPE), ("pages", 1 << 29, sa.SA_ERR_SHAPE),
+])
+def test_bad_descriptors(field, value, status):
+    d = desc(**{field: value})
+    assert set(calls(d).values()) == {status}
+    assert sa.sa_cache4_pool_bytes(d) == 0 and sa.sa_cache4_workspace_bytes(d, sa.SA_OP_CACHE4_DECODE, 1) == 0
+
+
+@pytest.mark.parametrize("arg", "K V table pool q lens Y parents refs table_out lens_out refs_out keep add info".split())
+def test_null_arguments(arg):
+    got = calls(desc(), **{arg: None})
+    assert got and set(got.values()) == {sa.SA_ERR_NULL}
+
+
+@pytest.mark.parametrize("arg", "K V pool q Y ws".split())
+def test_addresses_off_the_16_byte_grid(arg):
+    got = calls(desc(), **{arg: C.c_void_p(4096 + 8)})
+    assert got and set(got.values()) == {sa.SA_ERR_UNSUPPORTED}
+
+
+@pytest.mark.parametrize("arg", "table lens LSE starts counts parents refs table_out lens_out keep add info".split())
+def test_addresses_off_the_4_byte_grid(arg):
+    got = calls(desc(), **{arg: C.c_void_p(4096 + 2)})
+    assert got and set(got.values()) == {sa.SA_ERR_UNSUPPORTED}
+
+
+def test_token_counts_and_lengths():
+    for T in (0, -1):
+        assert set(calls(desc(), T=T).values()) == {sa.SA_ERR_SHAPE}
+        assert sa.sa_cache4_workspace_bytes(desc(), sa.SA_OP_CACHE4_DECODE, T) == 0
+    assert set(calls(desc(), T=1 << 28).values()) == {sa.SA_ERR_SHAPE}  # 2 * 8 * 2^28 rows
+    for n in (0, -5, 16 * 64 + 1):
+        assert set(calls(desc(), max_len=n).values()) == {sa.SA_ERR_SHAPE}
+    assert set(calls(desc(), max_moves=-1).values()) == {sa.SA_ERR_SHAPE}
+
+
+def test_workspaces():
+    d = desc(B=1, Hq=32, Hkv=8, max_pages=512, pages=512)
+    need = sa.sa_cache4_workspace_bytes(d, sa.SA_OP_CACHE4_DECODE, 1)
+    assert need > 0
+    for op, name in ((sa.SA_OP_CACHE4_DECODE, "sa_cache4_decode_fwd"), (sa.SA_OP_PAGES_EXTEND, "sa_pages_extend"),
+                     (sa.SA_OP_PAGES_COMPACT, "sa_pages_compact")):
+        need = sa.sa_cache4_workspace_bytes(d, op, 5)
+        assert need > 0 and calls(d, ws_bytes=need - 1)[name] == sa.SA_ERR_WORKSPACE and calls(d, ws=None)[name] == sa.SA_ERR_WORKSPACE
+    assert sa.sa_cache4_workspace_bytes(d, 99, 1) == 0
+
+
+def test_outputs_that_overlap_inputs():
+    d = desc()
+    name = "sa_pages_fork"
+    assert calls(d, table_out=FAKE)[name] == sa.SA_ERR_UNSUPPORTED
+    assert calls(d, table_out=C.c_void_p(4096 + 2 * 16 * 4 - 4))[name] == sa.SA_ERR_UNSUPPORTED
+    assert calls(d, lens_out=C.c_void_p(4096 + 4))[name] == sa.SA_ERR_UNSUPPORTED
+    assert calls(d, refs_out=C.c_void_p(4096 - 4))[name] == sa.SA_ERR_UNSUPPORTED
+    name = "sa_pages_compact"
+    assert calls(d, table_out=C.c_void_p(4096 + 4))[name] == sa.SA_ERR_UNSUPPORTED
+    assert calls(d, refs_out=C.c_void_p(4096 + 39 * 4))[name] == sa.SA_ERR_UNSUPPORTED
+
+
+def test_pool_size():
+    assert sa.sa_cache4_pool_bytes(desc()) == 3 * 40 * 2 * 2 * 34 * 128
+    # a quarter of the bf16 rows, and a sixteenth of that for the scales
+    assert 34 * 128 * 16 == 17 * (2 * 32 * 128 * 2) // 4
+
+
+def test_binding_raises_with_status():
+    import torch
+    x = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16)
+    t = torch.zeros(1, 1, dtype=torch.int32)
+    with pytest.raises(sa.SaError) as e:
+        sa.sa_cache4_write(desc(d=32), x, x, None, None, t, x)
+    assert e.value.status == sa.SA_ERR_UNSUPPORTED and "sa_cache4_write" in str(e.value)
