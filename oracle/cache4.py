@@ -6,13 +6,13 @@ import numpy as np
 
 MAGNITUDES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
 TILE = 32
-NO_ROW, LEAST = 255, 2
+NO_ROW, ONE = 255, 127
 
 
 def block_exponent(amax: float) -> int:
     """e of 2^e for a block of 32 whose largest magnitude is amax (finite)"""
     if amax == 0:
-        return -125
+        return 0
     e = math.frexp(amax)[1] - 1 - 2   # floor(log2 amax) - 2
     if amax / 2.0 ** e > 7:
         e += 1
@@ -34,7 +34,7 @@ def quantise_row(k, v):
     """One row of K and of V of one head -> (codes, bytes) of each"""
     bad = not (np.isfinite(k).all() and np.isfinite(v).all())
     out = []
-    for x, mark in ((k, NO_ROW), (v, LEAST)):
+    for x, mark in ((k, NO_ROW), (v, ONE)):
         d = len(x)
         if bad:
             out.append(([0] * d, [mark] * (d // 32)))

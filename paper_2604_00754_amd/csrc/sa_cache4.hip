@@ -138,11 +138,11 @@ struct Elements<float, E> {
 };
 
 // The scale byte of a block whose largest magnitude has the bits `top`: its exponent less 2, one more past 1.75 (7/4) of the power.
+constexpr uint32_t kNoRow = 255, kOne = 127;
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   const int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return (uint32_t)(e < 2 ? 2 : e);
+  return top == 0 ? kOne : (uint32_t)(e < 2 ? 2 : e);
 }
-constexpr uint32_t kNoRow = 255, kLeast = 2;
 
 struct RowsArgs {
   Cache c;
@@ -217,7 +217,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
     vs[j] = scale_byte(vt);
     kc[j] = k[j].codes(__uint_as_float(ks[j] << 23));
     vc[j] = v[j].codes(__uint_as_float(vs[j] << 23));
-    if (bad) { kc[j] = 0; vc[j] = 0; ks[j] = kNoRow; vs[j] = kLeast; }
+    if (bad) { kc[j] = 0; vc[j] = 0; ks[j] = kNoRow; vs[j] = kOne; }
   }
   bool all = true;
 #pragma unroll
@@ -374,22 +374,39 @@ struct AttnArgs {
   float scale_log2e;
 };
 
+// The maximum is raised where a score passes it by more than this; the largest probability is then 2^15, with the lift, and the smallest
+// that f16 holds to all its bits 2^-21 of the largest possible.
+constexpr float kRaise = 8.f, kLift = 7.f;
+
 __device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
 
-// x as PARTS bf16 numbers whose sum is x to 8, 17 or 24 bits, in the words w[part] of two elements
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+// x and y as PARTS numbers of 8 (bf16) or 11 bits (f16) whose sums they are to PARTS times as many, in the words w[part]
 template <int PARTS>
-__device__ __forceinline__ void split_pair(float x, float y, uint32_t* w) {
+__device__ __forceinline__ void split_pair_bf16(float x, float y, uint32_t* w) {
 #pragma unroll
   for (int p = 0; p < PARTS; ++p) {
     w[p] = pack_bf16(x, y);
-    if (p + 1 < PARTS) {
-      x -= bf16lo(w[p]);
-      y -= bf16hi(w[p]);
-    }
+    x -= bf16lo(w[p]);
+    y -= bf16hi(w[p]);
+  }
+}
+template <int PARTS>
+__device__ __forceinline__ void split_pair_f16(float x, float y, uint32_t* w) {
+#pragma unroll
+  for (int p = 0; p < PARTS; ++p) {
+    const f32x2 v = {x, y};
+    const f16x2 h = __builtin_convertvector(v, f16x2);
+    w[p] = __builtin_bit_cast(uint32_t, h);
+    x -= (float)h[0];
+    y -= (float)h[1];
   }
 }
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+__device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
 constexpr int kAttnWaves = 4;
 
@@ -399,42 +416,87 @@ struct TileRegs {
   uint32_t v[D / 16];     // D = 128: a word per row j; D = 64: rows 2j, 2j + 1 share one
   uint32_t ks;            // scale bytes of the halves
   u32x2 vs;               // of rows j
-  __device__ __forceinline__ void load(const unsigned char* base, int r, int g) {
+  __device__ __forceinline__ void load_k(const unsigned char* base, int r, int g) {
     using L = Tile<D>;
-    const unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
-    if constexpr (D == 128) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(base + (16 * h + r) * 64 + 16 * g);
+    for (int h = 0; h < 2; ++h) {
+      const unsigned char* kp = base + (uint32_t)((16 * h + r) * (D / 2) + (D / 8) * g);
+      if constexpr (D == 128) {
+        const u32x4 x = *reinterpret_cast<const u32x4*>(kp);
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[h][i] = x[i];
-      }
-      const u32x4 a = reinterpret_cast<const u32x4*>(vp)[0], b = reinterpret_cast<const u32x4*>(vp)[1];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
-      ks = *reinterpret_cast<const uint16_t*>(base + L::kKs + (g * 16 + r) * 2);
-    } else {
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(base + (16 * h + r) * 32 + 8 * g);
+      } else {
+        const u32x2 x = *reinterpret_cast<const u32x2*>(kp);
         k[h][0] = x[0]; k[h][1] = x[1];
       }
-      const u32x4 a = *reinterpret_cast<const u32x4*>(vp);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = a[i];
-      ks = *reinterpret_cast<const uint16_t*>(base + L::kKs + ((g >> 1) * 16 + r) * 2);
     }
-    vs = *reinterpret_cast<const u32x2*>(base + L::kVs + ((r / L::LPB) * 4 + g) * 8);
+    ks = *reinterpret_cast<const uint16_t*>(base + (uint32_t)(L::kKs + ((g * (D / 32) / 4) * 16 + r) * 2));
+  }
+  __device__ __forceinline__ void load_v(const unsigned char* base, int r, int g) {
+    using L = Tile<D>;
+#pragma unroll
+    for (int w = 0; w < D / 64; ++w) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>(base + (uint32_t)(L::kV + (g * 16 + r) * 8 * L::RB + 16 * w));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[4 * w + i] = x[i];
+    }
+    vs = *reinterpret_cast<const u32x2*>(base + (uint32_t)(L::kVs + ((r / L::LPB) * 4 + g) * 8));
   }
 };
 
-template <int SEL>
+// the two elements of a byte of the word, as pairs of V (bf16x8: bf16, f16x8: f16)
+template <typename V, int SEL>
 __device__ __forceinline__ uint32_t two_values(uint32_t codes, float scale) {
-  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+  if constexpr (sizeof(V) == sizeof(bf16x8) && __is_same(V, bf16x8)) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+  else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, SEL));
+}
+template <typename V>
+__device__ __forceinline__ uint32_t two_values_of(uint32_t codes, float scale, int sel) {  // sel: known after unrolling
+  return sel == 0 ? two_values<V, 0>(codes, scale) : sel == 1 ? two_values<V, 1>(codes, scale) : sel == 2 ? two_values<V, 2>(codes, scale) : two_values<V, 3>(codes, scale);
 }
 __device__ __forceinline__ bf16x8 eight_values(uint32_t codes, float scale) {
-  const u32x4 w = {two_values<0>(codes, scale), two_values<1>(codes, scale), two_values<2>(codes, scale), two_values<3>(codes, scale)};
+  const u32x4 w = {two_values<bf16x8, 0>(codes, scale), two_values<bf16x8, 1>(codes, scale), two_values<bf16x8, 2>(codes, scale), two_values<bf16x8, 3>(codes, scale)};
   return __builtin_bit_cast(bf16x8, w);
+}
+
+// O^T += V^T P^T over the 8 rows of each lane group, for every block of query rows.  V is the operand type: f16 with P in PARTS of 11
+// bits, or bf16 with parts of 8 where a scale of the tile is out of f16's reach.  p: the probabilities, rows 4 half + i.
+template <typename V, int D, int NT, int PARTS>
+__device__ __forceinline__ void add_pv(const uint32_t* v, const float* vscale, const float (*p)[8], f32x4 (*o)[D / 16]) {
+  V pf[NT][PARTS];
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    u32x4 w[PARTS];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t parts[PARTS];
+      if constexpr (__is_same(V, bf16x8)) split_pair_bf16<PARTS>(p[n][2 * i], p[n][2 * i + 1], parts);
+      else split_pair_f16<PARTS>(p[n][2 * i], p[n][2 * i + 1], parts);
+#pragma unroll
+      for (int k = 0; k < PARTS; ++k) w[k][i] = parts[k];
+    }
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) pf[n][k] = __builtin_bit_cast(V, w[k]);
+  }
+#pragma unroll
+  for (int q = 0; q < D / 32; ++q) {
+    uint32_t pr[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pr[j] = D == 128 ? two_values_of<V>(v[j], vscale[j], q) : two_values_of<V>(v[j / 2], vscale[j], 2 * (j & 1) + q);
+    u32x4 lo, hi;  // blocks 2q and 2q + 1, rows in pairs
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
+      hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int k = PARTS - 1; k >= 0; --k) {
+        o[n][2 * q] = mfma16(__builtin_bit_cast(V, lo), pf[n][k], o[n][2 * q]);
+        o[n][2 * q + 1] = mfma16(__builtin_bit_cast(V, hi), pf[n][k], o[n][2 * q + 1]);
+      }
+  }
 }
 
 template <typename T>
@@ -455,18 +517,21 @@ __device__ __forceinline__ void load_q8<float>(const float* p, float (&x)[8]) {
 __device__ __forceinline__ void store_y(bf16_t* p, float v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
 __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 
+// Wavefronts a SIMD that the registers are kept for: what the compiler reaches without spilling.
+constexpr int attn_waves_per_simd(bool bf16, int D, int NT) { return NT == 1 ? (bf16 ? 4 : 3) : NT == 2 ? (D == 64 ? 3 : 2) : D == 64 && bf16 ? 2 : 1; }
+
 template <typename T, int D, int NT>
-__global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT)) void cache4_attn_kernel(AttnArgs a) {
   using L = Tile<D>;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of q
-  constexpr int PP = sizeof(T) == 2 ? 2 : 3;   // and of a probability
+  constexpr int PP = sizeof(T) == 2 ? 1 : 2;   // f16 parts of a probability (one bf16 part more)
   constexpr int KS = D / 32;                   // steps of the score product
   constexpr int DB = D / 16;                   // blocks of 16 elements
   constexpr int LD = D + 4;                    // floats between rows of the merge area
   __shared__ __align__(16) float lds_o[kAttnWaves][16][LD];
   __shared__ float lds_ml[kAttnWaves][16][2];
 
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int split = (int)(blockIdx.x % (unsigned)a.splits);
   const unsigned rest = blockIdx.x / (unsigned)a.splits;
   const int rb = (int)(rest % (unsigned)a.row_blocks);
@@ -499,7 +564,7 @@ __global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t p[QP];
-        split_pair<QP>(x[2 * i], x[2 * i + 1], p);
+        split_pair_bf16<QP>(x[2 * i], x[2 * i + 1], p);
 #pragma unroll
         for (int k = 0; k < QP; ++k) w[k][i] = p[k];
       }
@@ -510,6 +575,12 @@ __global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a
 
   f32x4 o[NT][DB];
   float m[NT], l[NT];
+  const int t0 = split * a.chunk, t1 = min(t0 + a.chunk, most < 0 ? 0 : most / kTile + 1);
+  // The wave's tiles, with V as operands of the type of `kind`; false if a tile's scales are out of f16's reach.
+  auto walk = [&](auto kind) -> bool {
+    using Operand = decltype(kind);
+    constexpr bool kHalf = __is_same(Operand, f16x8);
+    uint32_t unfit = 0;
 #pragma unroll
   for (int n = 0; n < NT; ++n) {
 #pragma unroll
@@ -517,27 +588,31 @@ __global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a
     m[n] = -INFINITY;
     l[n] = 0.f;
   }
-
-  const int t0 = split * a.chunk, t1 = min(t0 + a.chunk, most < 0 ? 0 : most / kTile + 1);
   for (int first = t0 + wave; first < t1; first += 64 * kAttnWaves) {
     // the page table's entries of the wave's next 64 tiles, one a lane
     const int mine = first + kAttnWaves * lane;
     const int numbers = mine < t1 ? tile_number(a.c, b, hk, mine) : -1;
     const int turns = min(64, (t1 - first + kAttnWaves - 1) / kAttnWaves);
-    for (int i = 0; i < turns; ++i) {
+    TileRegs<D> x;
+    auto place = [&](int i) {  // (a tile that is not there: any other in its place, not looked at)
       const int number = __builtin_amdgcn_readlane(numbers, i);
-      if (number < 0) continue;
+      return a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes;
+    };
+    x.load_k(place(0), r, g);
+    __builtin_amdgcn_sched_barrier(0);  // (in the loop's order: the waits at its top count the loads behind K's)
+    x.load_v(place(0), r, g);
+    __builtin_amdgcn_sched_barrier(0);
+    for (int i = 0; i < turns; ++i) {
+      const bool there = __builtin_amdgcn_readlane(numbers, i) >= 0;
+      const unsigned char* next = place(min(i + 1, turns - 1));  // (the last turn asks for its own again: the loads need no branch)
       const int tile = first + kAttnWaves * i;
-      TileRegs<D> x;
-      x.load(a.c.pool + (size_t)number * L::kBytes, r, g);
-
       const bool partly = tile * kTile + kTile - 1 > least;  // some query row does not see all of it
-      // scores
-      f32x4 sc[NT][2];
+      // scores; K's registers are free for the next tile after them, V's after the second product
+      float p[NT][8];
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-        const float s = __uint_as_float(((x.ks >> (8 * h)) & 0xffu) << 23);
-        const float scale = ((x.ks >> (8 * h)) & 0xffu) == kNoRow ? __uint_as_float(0x7fc00000u) : s;
+        const uint32_t byte = (x.ks >> (8 * h)) & 0xffu;
+        const float scale = __uint_as_float(byte == kNoRow ? 0x7fc00000u : byte << 23);
         bf16x8 kf[KS];
 #pragma unroll
         for (int st = 0; st < KS; ++st) kf[st] = eight_values(x.k[h][st], scale);
@@ -548,84 +623,64 @@ __global__ __launch_bounds__(kAttnWaves * 64) void cache4_attn_kernel(AttnArgs a
           for (int k = QP - 1; k >= 0; --k)
 #pragma unroll
             for (int st = 0; st < KS; ++st) acc = mfma16(kf[st], qf[n][st][k], acc);
-          sc[n][h] = acc;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) p[n][4 * h + e] = acc[e];
         }
       }
-      bf16x8 p[NT][PP];
+      __builtin_amdgcn_sched_barrier(0);
+      x.load_k(next, r, g);
+      if (there) {
+        if (partly) {
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float top = -INFINITY;
+          for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+            for (int j = 0; j < 8; ++j)
+              if (tile * kTile + L::row(g, j) > last[n]) p[n][j] = -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            float s = sc[n][h][e] * a.scale_log2e;
-            if (partly && tile * kTile + 16 * h + 4 * g + e > last[n]) s = -INFINITY;
-            sc[n][h][e] = s;
-            top = fmaxf(top, s);
-          }
-        if (__any(top > m[n] + 8.f)) {   // (m = -inf at first)
-          float mn = fmaxf(top, __shfl_xor(top, 16));
-          mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
-          const float corr = exp2_above(m[n], mn);
-          l[n] *= corr;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) o[n][d] *= corr;
-          m[n] = mn;
+          for (int j = 0; j < 8; ++j)  // never written: whatever lies there is kept finite
+            if (tile * kTile + L::row(g, j) >= len) x.vs[j / 4] = (x.vs[j / 4] & ~(0xffu << (8 * (j & 3)))) | kOne << (8 * (j & 3));
         }
-        const float ref = m[n] == -INFINITY ? 0.f : m[n];
-        u32x4 w[PP];
+        if constexpr (kHalf) {
+          // bytes 108..139, 2^-19 .. 2^12: every value of the block is an f16 number (a byte that overflows its sum fails by itself)
+          const uint32_t off = ((x.vs[0] + 0x14141414u) ^ 0x80808080u) | ((x.vs[1] + 0x14141414u) ^ 0x80808080u);
+          unfit |= off & 0xe0e0e0e0u;
+        }
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int n = 0; n < NT; ++n) {
+          float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7])));
+          top *= a.scale_log2e;
+          if (__any(top > m[n] + kRaise)) {   // (m = -inf at first)
+            float mn = fmaxf(top, __shfl_xor(top, 16));
+            mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
+            const float corr = exp2_above(m[n], mn);
+            l[n] *= corr;
 #pragma unroll
-          for (int e = 0; e < 4; e += 2) {
-            const float p0 = exp2f(sc[n][h][e] - ref), p1 = exp2f(sc[n][h][e + 1] - ref);
-            l[n] += p0 + p1;
-            uint32_t parts[PP];
-            split_pair<PP>(p0, p1, parts);
-#pragma unroll
-            for (int k = 0; k < PP; ++k) w[k][2 * h + e / 2] = parts[k];
+            for (int d = 0; d < DB; ++d) o[n][d] *= corr;
+            m[n] = mn;
           }
+          const float ref = m[n] == -INFINITY ? 0.f : kLift - m[n];
 #pragma unroll
-        for (int k = 0; k < PP; ++k) p[n][k] = __builtin_bit_cast(bf16x8, w[k]);
-      }
-      // V: words of rows j -> operands of blocks 2q, 2q + 1, rows in pairs
-      float vsc[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        uint32_t byte = (x.vs[j / 4] >> (8 * (j & 3))) & 0xffu;
-        if (partly && tile * kTile + L::row(g, j) >= len) byte = 0;  // never written: whatever lies there is kept finite
-        vsc[j] = __uint_as_float(byte << 23);
-      }
-#pragma unroll
-      for (int q = 0; q < DB / 2; ++q) {
-        uint32_t pr[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          if constexpr (D == 128) {
-            pr[j] = q == 0 ? two_values<0>(x.v[j], vsc[j]) : q == 1 ? two_values<1>(x.v[j], vsc[j]) : q == 2 ? two_values<2>(x.v[j], vsc[j]) : two_values<3>(x.v[j], vsc[j]);
-          } else {
-            pr[j] = (j & 1) ? (q ? two_values<3>(x.v[j / 2], vsc[j]) : two_values<2>(x.v[j / 2], vsc[j]))
-                            : (q ? two_values<1>(x.v[j / 2], vsc[j]) : two_values<0>(x.v[j / 2], vsc[j]));
+          for (int j = 0; j < 8; ++j) {
+            p[n][j] = __builtin_amdgcn_exp2f(fmaf(p[n][j], a.scale_log2e, ref));
+            l[n] += p[n][j];
           }
         }
-        u32x4 lo, hi;
+        __builtin_amdgcn_sched_barrier(0);
+        float vscale[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          lo[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x05040100u);
-          hi[j] = __builtin_amdgcn_perm(pr[2 * j + 1], pr[2 * j], 0x07060302u);
-        }
-        const bf16x8 flo = __builtin_bit_cast(bf16x8, lo), fhi = __builtin_bit_cast(bf16x8, hi);
-#pragma unroll
-        for (int n = 0; n < NT; ++n)
-#pragma unroll
-          for (int k = PP - 1; k >= 0; --k) {
-            o[n][2 * q] = mfma16(flo, p[n][k], o[n][2 * q]);
-            o[n][2 * q + 1] = mfma16(fhi, p[n][k], o[n][2 * q + 1]);
-          }
+        for (int j = 0; j < 8; ++j) vscale[j] = __uint_as_float(((x.vs[j / 4] >> (8 * (j & 3))) & 0xffu) << 23);
+        add_pv<Operand, D, NT, kHalf ? PP : PP + 1>(x.v, vscale, p, o);
       }
+      __builtin_amdgcn_sched_barrier(0);
+      x.load_v(next, r, g);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
+    return !__any(unfit != 0);
+  };
+  if (!walk(f16x8{})) walk(bf16x8{});
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n] -= kLift;  // what the sums are relative to
 
   // the waves' results, 16 query rows at a time
 #pragma unroll

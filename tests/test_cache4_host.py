@@ -26,7 +26,7 @@ def test_ties_go_to_the_even_code_and_the_scale_turns_at_seven():
     assert codes == [0, 2, 2, 4, 4, 6, 6, 7]
     assert orc.block_exponent(7.0) == 0 and orc.block_exponent(np.nextafter(7.0, 8)) == 1
     assert orc.block_exponent(4.0) == 0 and orc.block_exponent(np.nextafter(4.0, 0)) == 0  # 3.99.. / 2^-1 > 7
-    assert orc.block_exponent(3.5) == -1 and orc.block_exponent(2.0 ** -149) == -125 and orc.block_exponent(0.0) == -125
+    assert orc.block_exponent(3.5) == -1 and orc.block_exponent(2.0 ** -149) == -125 and orc.block_exponent(0.0) == 0
 
 
 def test_normal_rows_are_held_as_well_as_the_better_of_two_powers_holds_them():

@@ -47,7 +47,7 @@ class Setup:
     def write(self, K, V, starts=None, counts=None, table=None):
         """On both sides; K, V: pairs as from rows()"""
         T = K[1].shape[2]
-        self.vmax = max(self.vmax, 1.2 * np.abs(V[1][np.isfinite(V[1])]).max())  # rounding raises a block's largest by a fifth at most
+        self.vmax = max(self.vmax, 1.2 * np.abs(V[1][np.isfinite(V[1])]).max(initial=0))  # rounding raises a block's largest by a fifth at most
         table = self.table if table is None else table
         s, c = (None if x is None else self.dev(np.asarray(x, np.int32)) for x in (starts, counts))
         sa().sa_cache4_write(self.desc, K[0], V[0], s, c, self.dev(table), self.pool)
@@ -242,6 +242,24 @@ def test_scores_far_apart_and_a_given_scale(dtype):
     c.write(K, V)
     c.check(3, [256])
     c.check(1, [130])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sizes", [(2.0 ** -19, 1.0), (2.0 ** -21, 2.0 ** -17), (2.0 ** 13, 2.0 ** 10), (2.0 ** 16, 2.0 ** 16), (1e-30, 1e30), (2.0 ** -120, 0.0)])
+def test_values_of_any_size(dtype, d, sizes):
+    """Scales of V on either side of what f16 holds (2^-19 .. 2^12), the sizes in turn from tile to tile and zeros between: the bound is
+    relative to the largest value seen"""
+    c = Setup(1, 4, 1, d, 32, 8, dtype, seed=d)
+    K = c.rows(250)
+    V = c.rng.standard_normal((1, 1, 250, d)).astype(np.float32)
+    V *= np.resize(np.repeat(np.float32(sizes), 32), 250)[:, None]
+    V[0, 0, 40:50] = 0
+    V = (c.dev(V),)
+    c.write(K, (V[0], U.to_np64(V[0])))
+    c.assert_bytes()
+    c.check(1, [250])
+    c.check(20, [250])
 
 
 def test_one_cached_row_comes_back_as_it_is():
