@@ -74,10 +74,6 @@ struct Elements<bf16_t, E> {
       w[0] = x[0]; w[1] = x[1];
     }
   }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) w[i] = 0;
-  }
   // largest magnitude as the bits of an fp32 number (an infinity or NaN is above all others)
   __device__ __forceinline__ uint32_t top() const {
     uint32_t m = 0;
@@ -111,10 +107,6 @@ struct Elements<float, E> {
 #pragma unroll
       for (int k = 0; k < 4; ++k) x[i + k] = v[k];
     }
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = 0.f;
   }
   __device__ __forceinline__ uint32_t top() const {
     uint32_t m = 0;
@@ -155,30 +147,27 @@ struct RowsArgs {
 
 // What a wave of the two row kernels works on: the rows t0 + row(g, j) of one sequence and head that lie in one tile.
 struct Rows {
-  int b, hk, tile;
-  long t0;        // t of the tile's first row
+  int b, hk, tile;  // tile: -1 outside the sequence's positions
+  long t0;          // t of the tile's first row
   int count;
-  bool any;
+  bool any, whole;  // whether rows of the tile are among them, and all
 };
-template <int WAVES>
+constexpr int kRowWaves = 4;
 __device__ __forceinline__ Rows rows_of_wave(const RowsArgs& a) {
   Rows w;
-  const long work = (long)blockIdx.x * WAVES + (threadIdx.x >> 6);
-  const int k = (int)(work % a.tiles);
-  const long bh = work / a.tiles;
-  w.any = bh < (long)a.c.B * a.c.Hkv;
-  w.hk = (int)(bh % a.c.Hkv);
-  w.b = w.any ? (int)(bh / a.c.Hkv) : 0;
-  const int start = a.starts ? a.starts[w.b] : 0;
-  w.count = a.counts ? min(max(a.counts[w.b], 0), a.T) : a.T;
+  const unsigned blocks = (unsigned)(a.tiles + kRowWaves - 1) / kRowWaves, bh = blockIdx.x / blocks;
+  const int k = (int)(blockIdx.x % blocks) * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  w.hk = (int)(bh % (unsigned)a.c.Hkv);
+  w.b = (int)(bh / (unsigned)a.c.Hkv);
+  const int start = a.starts ? __builtin_amdgcn_readfirstlane(a.starts[w.b]) : 0;
+  w.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[w.b], 0), a.T)) : a.T;
   const long tile = (long)(start >> 5) + k;
   w.t0 = tile * kTile - start;
-  w.any = w.any && w.t0 < w.count;
+  w.any = k < a.tiles && w.t0 < w.count;
+  w.whole = w.t0 >= 0 && w.t0 + kTile <= w.count;
   w.tile = tile < 0 || tile * kTile >= a.c.capacity ? -1 : (int)tile;
   return w;
 }
-
-constexpr int kRowWaves = 4;
 
 // One wave per tile that the rows touch, 8 rows a lane group, K and V of a row by the same lanes: a row that holds an infinity or
 // NaN in either is marked in both.  Bound: HBM (reads 4 d bytes a row in bf16, writes 17/16 d).
@@ -186,28 +175,26 @@ template <typename T, int D>
 __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a) {
   using L = Tile<D>;
   constexpr int E = L::E;
-  const Rows w = rows_of_wave<kRowWaves>(a);
+  const Rows w = rows_of_wave(a);
   if (!w.any || w.tile < 0) return;
-  const int number = tile_number(a.c, w.b, w.hk, w.tile);
+  const int number = __builtin_amdgcn_readfirstlane(tile_number(a.c, w.b, w.hk, w.tile));
   if (number < 0) return;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   unsigned char* base = a.c.pool + (size_t)number * L::kBytes;
   const size_t src = ((size_t)w.b * a.c.Hkv + w.hk) * a.T;
   Elements<T, E> k[8], v[8];
   bool in[8];
+  const T* kr = reinterpret_cast<const T*>(a.K) + src * D + r * E;
+  const T* vr = reinterpret_cast<const T*>(a.V) + src * D + r * E;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 8; ++j) {  // (rows of the tile that are not written: the first or last that is in their place)
     const long t = w.t0 + L::row(g, j);
     in[j] = t >= 0 && t < w.count;
-    if (in[j]) {
-      const size_t at = (src + (size_t)t) * D + r * E;
-      k[j].load(reinterpret_cast<const T*>(a.K) + at);
-      v[j].load(reinterpret_cast<const T*>(a.V) + at);
-    } else {
-      k[j].clear();
-      v[j].clear();
-    }
+    const size_t at = (size_t)(t < 0 ? 0 : t < w.count ? t : w.count - 1) * D;
+    k[j].load(kr + at);
+    v[j].load(vr + at);
   }
+  __builtin_amdgcn_sched_barrier(0);  // all loads in flight together
   uint32_t kc[8], vc[8], ks[8], vs[8];
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -217,21 +204,25 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
     vs[j] = scale_byte(vt);
     kc[j] = k[j].codes(__uint_as_float(ks[j] << 23));
     vc[j] = v[j].codes(__uint_as_float(vs[j] << 23));
-    if (bad) { kc[j] = 0; vc[j] = 0; ks[j] = kNoRow; vs[j] = kOne; }
+    kc[j] = bad ? 0 : kc[j];
+    vc[j] = bad ? 0 : vc[j];
+    ks[j] = bad ? kNoRow : ks[j];
+    vs[j] = bad ? kOne : vs[j];
   }
-  bool all = true;
-#pragma unroll
-  for (int j = 0; j < 8; ++j) all = all && in[j];
-  // K codes: rows as they are; V codes: the 8 rows of a lane group side by side
+  // K codes: rows as they are; V codes: the 8 rows of a lane group side by side; scales: by the first lane of a block
+  unsigned char* kp = base + (4 * g) * (D / 2) + r * L::RB;
   unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
+  const int c = r / L::LPB;
+  unsigned char* kq = base + L::kKs + (c * 16 + 4 * g) * 2;
+  unsigned char* vq = base + L::kVs + (c * 4 + g) * 8;
+  const auto put_k = [&](int j) {
+    unsigned char* to = kp + L::row(0, j) * (D / 2);
+    if constexpr (L::RB == 4) *reinterpret_cast<uint32_t*>(to) = kc[j];
+    else *reinterpret_cast<uint16_t*>(to) = (uint16_t)kc[j];
+  };
+  if (w.whole) {
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
-    if (in[j]) {
-      unsigned char* kp = base + L::row(g, j) * (D / 2) + r * L::RB;
-      if constexpr (L::RB == 4) *reinterpret_cast<uint32_t*>(kp) = kc[j];
-      else *reinterpret_cast<uint16_t*>(kp) = (uint16_t)kc[j];
-    }
-  if (all) {
+    for (int j = 0; j < 8; ++j) put_k(j);
     if constexpr (L::RB == 4) {
       reinterpret_cast<u32x4*>(vp)[0] = u32x4{vc[0], vc[1], vc[2], vc[3]};
       reinterpret_cast<u32x4*>(vp)[1] = u32x4{vc[4], vc[5], vc[6], vc[7]};
@@ -239,30 +230,23 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
       *reinterpret_cast<u32x4*>(vp) = u32x4{(vc[0] & 0xffffu) | (vc[1] << 16), (vc[2] & 0xffffu) | (vc[3] << 16),
                                             (vc[4] & 0xffffu) | (vc[5] << 16), (vc[6] & 0xffffu) | (vc[7] << 16)};
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (in[j]) {
-        if constexpr (L::RB == 4) reinterpret_cast<uint32_t*>(vp)[j] = vc[j];
-        else reinterpret_cast<uint16_t*>(vp)[j] = (uint16_t)vc[j];
-      }
-  }
-  if (r % L::LPB == 0) {  // the first lane of a block keeps its scales
-    const int c = r / L::LPB;
-    unsigned char* kq = base + L::kKs + (c * 16 + 4 * g) * 2;
-    unsigned char* vq = base + L::kVs + (c * 4 + g) * 8;
-    if (all) {
+    if (r % L::LPB == 0) {
       *reinterpret_cast<u32x2*>(kq) = u32x2{ks[0] | ks[4] << 8 | ks[1] << 16 | ks[5] << 24, ks[2] | ks[6] << 8 | ks[3] << 16 | ks[7] << 24};
       *reinterpret_cast<u32x2*>(vq) = u32x2{vs[0] | vs[1] << 8 | vs[2] << 16 | vs[3] << 24, vs[4] | vs[5] << 8 | vs[6] << 16 | vs[7] << 24};
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (in[j]) {
-          kq[2 * (j & 3) + (j >> 2)] = (unsigned char)ks[j];
-          vq[j] = (unsigned char)vs[j];
-        }
     }
+    return;
   }
+#pragma unroll
+  for (int j = 0; j < 8; ++j)
+    if (in[j]) {
+      put_k(j);
+      if constexpr (L::RB == 4) reinterpret_cast<uint32_t*>(vp)[j] = vc[j];
+      else reinterpret_cast<uint16_t*>(vp)[j] = (uint16_t)vc[j];
+      if (r % L::LPB == 0) {
+        kq[2 * (j & 3) + (j >> 2)] = (unsigned char)ks[j];
+        vq[j] = (unsigned char)vs[j];
+      }
+    }
 }
 
 // E elements from their codes (low bytes of c), times the scale
@@ -309,9 +293,9 @@ __device__ __forceinline__ void store_values<float, 8>(float* p, uint32_t c, flo
 template <typename T, int D>
 __global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a) {
   using L = Tile<D>;
-  const Rows w = rows_of_wave<kRowWaves>(a);
+  const Rows w = rows_of_wave(a);
   if (!w.any) return;
-  const int number = w.tile < 0 ? -1 : tile_number(a.c, w.b, w.hk, w.tile);
+  const int number = w.tile < 0 ? -1 : __builtin_amdgcn_readfirstlane(tile_number(a.c, w.b, w.hk, w.tile));
   const bool there = number >= 0;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, c = r / L::LPB;
   const unsigned char* base = a.c.pool + (size_t)(there ? number : 0) * L::kBytes;
@@ -408,39 +392,45 @@ __device__ __forceinline__ void split_pair_f16(float x, float y, uint32_t* w) {
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 
-constexpr int kAttnWaves = 4;
 
+// A lane's part of a tile: loads through a buffer descriptor of the tile, whose base is scalar and whose offsets are four numbers a lane keeps.
+typedef __amdgpu_buffer_rsrc_t tile_buffer;
 template <int D>
 struct TileRegs {
   uint32_t k[2][D / 32];  // [half][word]: 8 elements a word
   uint32_t v[D / 16];     // D = 128: a word per row j; D = 64: rows 2j, 2j + 1 share one
   uint32_t ks;            // scale bytes of the halves
   u32x2 vs;               // of rows j
-  __device__ __forceinline__ void load_k(const unsigned char* base, int r, int g) {
+  int at_k, at_ks, at_v, at_vs;
+  __device__ __forceinline__ void place(int r, int g) {
     using L = Tile<D>;
+    at_k = r * (D / 2) + (D / 8) * g;
+    at_ks = L::kKs + ((g * (D / 32) / 4) * 16 + r) * 2;
+    at_v = L::kV + (g * 16 + r) * 8 * L::RB;
+    at_vs = L::kVs + ((r / L::LPB) * 4 + g) * 8;
+  }
+  __device__ __forceinline__ void load_k(tile_buffer t) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const unsigned char* kp = base + (uint32_t)((16 * h + r) * (D / 2) + (D / 8) * g);
       if constexpr (D == 128) {
-        const u32x4 x = *reinterpret_cast<const u32x4*>(kp);
+        const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(t, at_k, 16 * h * (D / 2), 0);
 #pragma unroll
         for (int i = 0; i < 4; ++i) k[h][i] = x[i];
       } else {
-        const u32x2 x = *reinterpret_cast<const u32x2*>(kp);
+        const u32x2 x = __builtin_amdgcn_raw_buffer_load_b64(t, at_k, 16 * h * (D / 2), 0);
         k[h][0] = x[0]; k[h][1] = x[1];
       }
     }
-    ks = *reinterpret_cast<const uint16_t*>(base + (uint32_t)(L::kKs + ((g * (D / 32) / 4) * 16 + r) * 2));
+    ks = __builtin_amdgcn_raw_buffer_load_b16(t, at_ks, 0, 0);
   }
-  __device__ __forceinline__ void load_v(const unsigned char* base, int r, int g) {
-    using L = Tile<D>;
+  __device__ __forceinline__ void load_v(tile_buffer t) {
 #pragma unroll
     for (int w = 0; w < D / 64; ++w) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>(base + (uint32_t)(L::kV + (g * 16 + r) * 8 * L::RB + 16 * w));
+      const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(t, at_v, 16 * w, 0);
 #pragma unroll
       for (int i = 0; i < 4; ++i) v[4 * w + i] = x[i];
     }
-    vs = *reinterpret_cast<const u32x2*>(base + (uint32_t)(L::kVs + ((r / L::LPB) * 4 + g) * 8));
+    vs = __builtin_amdgcn_raw_buffer_load_b64(t, at_vs, 0, 0);
   }
 };
 
@@ -520,16 +510,16 @@ __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 // Wavefronts a SIMD that the registers are kept for: what the compiler reaches without spilling.
 constexpr int attn_waves_per_simd(bool bf16, int D, int NT) { return NT == 1 ? (bf16 ? 4 : 3) : NT == 2 ? (D == 64 ? 3 : 2) : D == 64 && bf16 ? 2 : 1; }
 
-template <typename T, int D, int NT>
-__global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT)) void cache4_attn_kernel(AttnArgs a) {
+template <typename T, int D, int NT, int W>
+__global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT)) void cache4_attn_kernel(AttnArgs a) {
   using L = Tile<D>;
   constexpr int QP = sizeof(T) == 2 ? 1 : 3;   // bf16 parts of q
   constexpr int PP = sizeof(T) == 2 ? 1 : 2;   // f16 parts of a probability (one bf16 part more)
   constexpr int KS = D / 32;                   // steps of the score product
   constexpr int DB = D / 16;                   // blocks of 16 elements
   constexpr int LD = D + 4;                    // floats between rows of the merge area
-  __shared__ __align__(16) float lds_o[kAttnWaves][16][LD];
-  __shared__ float lds_ml[kAttnWaves][16][2];
+  __shared__ __align__(16) float lds_o[W][16][LD];
+  __shared__ float lds_ml[W][16][2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
   const int split = (int)(blockIdx.x % (unsigned)a.splits);
@@ -538,7 +528,11 @@ __global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2
   const int bh = (int)(rest / (unsigned)a.row_blocks);
   const int hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
   const int row0 = rb * 16 * NT;
-  const int len = min(max(a.lens[b], 0), a.max_len);
+  // The numbers of the wave's tiles (64 at most), one a lane: of every tile that the longest sequence could have, so that the page
+  // table's entries arrive together with the sequence's length and not behind it.
+  const int first = split * a.chunk + wave, end = min((split + 1) * a.chunk, (a.max_len + kTile - 1) / kTile);
+  const int numbers = first + W * lane < end ? tile_number(a.c, b, hk, first + W * lane) : -1;
+  const int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[b], 0), a.max_len));
 
   // the last position each of the lane's query rows sees (-1 or less: none), and their largest and smallest over the block
   int last[NT];
@@ -575,38 +569,35 @@ __global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2
 
   f32x4 o[NT][DB];
   float m[NT], l[NT];
-  const int t0 = split * a.chunk, t1 = min(t0 + a.chunk, most < 0 ? 0 : most / kTile + 1);
+  const int turns = max(0, (min(end, most < 0 ? 0 : most / kTile + 1) - first + W - 1) / W);
   // The wave's tiles, with V as operands of the type of `kind`; false if a tile's scales are out of f16's reach.
   auto walk = [&](auto kind) -> bool {
     using Operand = decltype(kind);
     constexpr bool kHalf = __is_same(Operand, f16x8);
     uint32_t unfit = 0;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n) {
 #pragma unroll
-    for (int d = 0; d < DB; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-    m[n] = -INFINITY;
-    l[n] = 0.f;
-  }
-  for (int first = t0 + wave; first < t1; first += 64 * kAttnWaves) {
-    // the page table's entries of the wave's next 64 tiles, one a lane
-    const int mine = first + kAttnWaves * lane;
-    const int numbers = mine < t1 ? tile_number(a.c, b, hk, mine) : -1;
-    const int turns = min(64, (t1 - first + kAttnWaves - 1) / kAttnWaves);
+      for (int d = 0; d < DB; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+      m[n] = -INFINITY;
+      l[n] = 0.f;
+    }
     TileRegs<D> x;
-    auto place = [&](int i) {  // (a tile that is not there: any other in its place, not looked at)
+    auto place = [&](int i) {  // (a tile that is not there: the first of the pool in its place, not seen)
       const int number = __builtin_amdgcn_readlane(numbers, i);
-      return a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes;
+      return __builtin_amdgcn_make_buffer_rsrc(a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes, 0, L::kBytes, 0x20000);
     };
-    x.load_k(place(0), r, g);
+    x.place(r, g);
+    if (turns == 0) return true;
+    x.load_k(place(0));
     __builtin_amdgcn_sched_barrier(0);  // (in the loop's order: the waits at its top count the loads behind K's)
-    x.load_v(place(0), r, g);
+    x.load_v(place(0));
     __builtin_amdgcn_sched_barrier(0);
     for (int i = 0; i < turns; ++i) {
       const bool there = __builtin_amdgcn_readlane(numbers, i) >= 0;
-      const unsigned char* next = place(min(i + 1, turns - 1));  // (the last turn asks for its own again: the loads need no branch)
-      const int tile = first + kAttnWaves * i;
-      const bool partly = tile * kTile + kTile - 1 > least;  // some query row does not see all of it
+      const tile_buffer next = place(min(i + 1, turns - 1));  // (the last turn asks for its own again: the loads need no branch)
+      const int tile = first + W * i;
+      const bool partly = tile * kTile + kTile - 1 > least || !there;  // some query row does not see all of it
       // scores; K's registers are free for the next tile after them, V's after the second product
       float p[NT][8];
 #pragma unroll
@@ -628,54 +619,51 @@ __global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2
         }
       }
       __builtin_amdgcn_sched_barrier(0);
-      x.load_k(next, r, g);
-      if (there) {
-        if (partly) {
+      x.load_k(next);
+      if (partly) {
 #pragma unroll
-          for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-              if (tile * kTile + L::row(g, j) > last[n]) p[n][j] = -INFINITY;
+          for (int j = 0; j < 8; ++j)
+            if (tile * kTile + L::row(g, j) > last[n] || !there) p[n][j] = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < 8; ++j)  // never written: whatever lies there is kept finite
-            if (tile * kTile + L::row(g, j) >= len) x.vs[j / 4] = (x.vs[j / 4] & ~(0xffu << (8 * (j & 3)))) | kOne << (8 * (j & 3));
+        for (int j = 0; j < 8; ++j)  // never written, or another tile's: whatever lies there is kept finite
+          if (tile * kTile + L::row(g, j) >= len || !there) x.vs[j / 4] = (x.vs[j / 4] & ~(0xffu << (8 * (j & 3)))) | kOne << (8 * (j & 3));
+      }
+      if constexpr (kHalf) {
+        // bytes 108..139, 2^-19 .. 2^12: every value of the block is an f16 number (a byte that overflows its sum fails by itself)
+        const uint32_t off = ((x.vs[0] + 0x14141414u) ^ 0x80808080u) | ((x.vs[1] + 0x14141414u) ^ 0x80808080u);
+        unfit |= off & 0xe0e0e0e0u;
+      }
+#pragma unroll
+      for (int n = 0; n < NT; ++n) {
+        float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7])));
+        top *= a.scale_log2e;
+        if (__any(top > m[n] + kRaise)) {   // (m = -inf at first)
+          float mn = fmaxf(top, __shfl_xor(top, 16));
+          mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
+          const float corr = exp2_above(m[n], mn);
+          l[n] *= corr;
+#pragma unroll
+          for (int d = 0; d < DB; ++d) o[n][d] *= corr;
+          m[n] = mn;
         }
-        if constexpr (kHalf) {
-          // bytes 108..139, 2^-19 .. 2^12: every value of the block is an f16 number (a byte that overflows its sum fails by itself)
-          const uint32_t off = ((x.vs[0] + 0x14141414u) ^ 0x80808080u) | ((x.vs[1] + 0x14141414u) ^ 0x80808080u);
-          unfit |= off & 0xe0e0e0e0u;
+        const float ref = m[n] == -INFINITY ? 0.f : kLift - m[n];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[n][j] = __builtin_amdgcn_exp2f(fmaf(p[n][j], a.scale_log2e, ref));
+          l[n] += p[n][j];
         }
-#pragma unroll
-        for (int n = 0; n < NT; ++n) {
-          float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7])));
-          top *= a.scale_log2e;
-          if (__any(top > m[n] + kRaise)) {   // (m = -inf at first)
-            float mn = fmaxf(top, __shfl_xor(top, 16));
-            mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
-            const float corr = exp2_above(m[n], mn);
-            l[n] *= corr;
-#pragma unroll
-            for (int d = 0; d < DB; ++d) o[n][d] *= corr;
-            m[n] = mn;
-          }
-          const float ref = m[n] == -INFINITY ? 0.f : kLift - m[n];
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            p[n][j] = __builtin_amdgcn_exp2f(fmaf(p[n][j], a.scale_log2e, ref));
-            l[n] += p[n][j];
-          }
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        float vscale[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vscale[j] = __uint_as_float(((x.vs[j / 4] >> (8 * (j & 3))) & 0xffu) << 23);
-        add_pv<Operand, D, NT, kHalf ? PP : PP + 1>(x.v, vscale, p, o);
       }
       __builtin_amdgcn_sched_barrier(0);
-      x.load_v(next, r, g);
+      float vscale[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vscale[j] = __uint_as_float(((x.vs[j / 4] >> (8 * (j & 3))) & 0xffu) << 23);
+      add_pv<Operand, D, NT, kHalf ? PP : PP + 1>(x.v, vscale, p, o);
+      __builtin_amdgcn_sched_barrier(0);
+      x.load_v(next);
       __builtin_amdgcn_sched_barrier(0);
     }
-  }
     return !__any(unfit != 0);
   };
   if (!walk(f16x8{})) walk(bf16x8{});
@@ -692,22 +680,23 @@ __global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int d = 0; d < DB; ++d) lds_o[wave][r][DB * (4 * g + i) + d] = o[n][d][i];
+      for (int d = 0; d < DB; d += 4)
+        *reinterpret_cast<f32x4*>(&lds_o[wave][r][DB * (4 * g + i) + d]) = f32x4{o[n][d][i], o[n][d + 1][i], o[n][d + 2][i], o[n][d + 3][i]};
     if (g == 0) {
       lds_ml[wave][r][0] = m[n];
       lds_ml[wave][r][1] = ls;
     }
     __syncthreads();
-    for (int idx = threadIdx.x; idx < 16 * D; idx += kAttnWaves * 64) {
+    const int valid = min(16, a.rows - row0 - 16 * n);
+    for (int idx = threadIdx.x; idx < valid * D; idx += W * 64) {
       const int c = idx / D, e = idx % D;
       const int row = row0 + 16 * n + c;
-      if (row >= a.rows) continue;
       float M = lds_ml[0][c][0];
 #pragma unroll
-      for (int w = 1; w < kAttnWaves; ++w) M = fmaxf(M, lds_ml[w][c][0]);
+      for (int w = 1; w < W; ++w) M = fmaxf(M, lds_ml[w][c][0]);
       float v = 0.f, sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < kAttnWaves; ++w) {
+      for (int w = 0; w < W; ++w) {
         const float f = exp2_above(lds_ml[w][c][0], M);
         v = fmaf(f, lds_o[w][c][e], v);
         sum = fmaf(f, lds_ml[w][c][1], sum);
@@ -728,27 +717,37 @@ __global__ __launch_bounds__(kAttnWaves * 64, attn_waves_per_simd(sizeof(T) == 2
   }
 }
 
-constexpr int kMergeWaves = 8;
-
-// One workgroup per query row joins the splits' results: each wave runs over its own with a running maximum.
-template <typename T, int D>
-__global__ __launch_bounds__(kMergeWaves * 64) void cache4_merge_kernel(const float* __restrict__ part, T* __restrict__ Y,
-                                                                         float* __restrict__ LSE, int splits) {
-  constexpr int EPL = D / 64, UM = 4;
-  __shared__ float lds_m[kMergeWaves], lds_l[kMergeWaves], lds_o[kMergeWaves][D];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const float* P = part + (size_t)blockIdx.x * splits * (D + 2);
+// Joins the splits' results of a query row, W waves a row (one of them: four rows a workgroup, nothing exchanged): a wave
+// runs over its own splits with a running maximum, several of them in flight.
+template <typename T, int D, int W>
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(const float* __restrict__ part, T* __restrict__ Y,
+                                                                             float* __restrict__ LSE, int splits, int rows) {
+  constexpr int EPL = D / 64, UM = 8;
+  __shared__ float lds_m[W], lds_l[W], lds_o[W][D];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int row = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (row >= rows) return;  // (W = 1)
+  const float* P = part + (size_t)row * splits * (D + 2);
   float m = -INFINITY, l = 0.f, o[EPL] = {};
-  for (int s0 = wave; s0 < splits; s0 += kMergeWaves * UM) {
+  for (int s0 = W == 1 ? 0 : wave; s0 < splits; s0 += W * UM) {
     float mx[UM], lx[UM], x[UM][EPL], mn = m;
 #pragma unroll
     for (int u = 0; u < UM; ++u) {
-      const int s = s0 + u * kMergeWaves;
-      const float* row = P + (size_t)min(s, splits - 1) * (D + 2);
-      mx[u] = s < splits ? row[D] : -INFINITY;
-      lx[u] = s < splits ? row[D + 1] : 0.f;
+      const int s = s0 + u * W;
+      const float* at = P + (size_t)min(s, splits - 1) * (D + 2);
+      mx[u] = at[D];
+      lx[u] = at[D + 1];
 #pragma unroll
-      for (int i = 0; i < EPL; ++i) x[u][i] = s < splits ? row[lane + 64 * i] : 0.f;
+      for (int i = 0; i < EPL; ++i) x[u][i] = at[lane + 64 * i];
+    }
+#pragma unroll
+    for (int u = 0; u < UM; ++u) {
+      if (s0 + u * W >= splits) {
+        mx[u] = -INFINITY;
+        lx[u] = 0.f;
+#pragma unroll
+        for (int i = 0; i < EPL; ++i) x[u][i] = 0.f;
+      }
       mn = fmaxf(mn, mx[u]);
     }
     const float corr = exp2_above(m, mn);
@@ -764,6 +763,12 @@ __global__ __launch_bounds__(kMergeWaves * 64) void cache4_merge_kernel(const fl
     }
     m = mn;
   }
+  if constexpr (W == 1) {
+#pragma unroll
+    for (int i = 0; i < EPL; ++i) store_y(Y + (size_t)row * D + lane + 64 * i, l == 0.f ? 0.f : o[i] / l);
+    if (lane == 0 && LSE) LSE[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < EPL; ++i) lds_o[wave][lane + 64 * i] = o[i];
   if (lane == 0) {
@@ -775,15 +780,15 @@ __global__ __launch_bounds__(kMergeWaves * 64) void cache4_merge_kernel(const fl
     const int e = threadIdx.x;
     float M = lds_m[0], sum = 0.f, v = 0.f;
 #pragma unroll
-    for (int w = 1; w < kMergeWaves; ++w) M = fmaxf(M, lds_m[w]);
+    for (int w = 1; w < W; ++w) M = fmaxf(M, lds_m[w]);
 #pragma unroll
-    for (int w = 0; w < kMergeWaves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const float f = exp2_above(lds_m[w], M);
       sum = fmaf(f, lds_l[w], sum);
       v = fmaf(f, lds_o[w][e], v);
     }
-    store_y(Y + (size_t)blockIdx.x * D + e, sum == 0.f ? 0.f : v / sum);
-    if (e == 0 && LSE) LSE[blockIdx.x] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+    store_y(Y + (size_t)row * D + e, sum == 0.f ? 0.f : v / sum);
+    if (e == 0 && LSE) LSE[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
   }
 }
 
@@ -799,33 +804,50 @@ Cache cache_of(const sa_cache4_desc* c, void* pool, const int32_t* table) {
   return k;
 }
 
-int row_tiles(long rows) { return rows > 32 ? 4 : rows > 16 ? 2 : 1; }
+// Blocks of 16 query rows a wave takes (fp32 rows of 128 at most two: four spill).
+int row_tiles(const sa_cache4_desc* c, int T) {
+  const long rows = (long)(c->Hq / c->Hkv) * T;
+  return rows <= 16 ? 1 : rows <= 32 || (c->dtype == SA_F32 && c->d == 128) ? 2 : 4;
+}
 
-// Workgroups wanted; a cache of `tiles` tiles read by `groups` workgroups otherwise is cut into that many pieces.
-constexpr long kWanted = 512;
-long splits_for(long groups, long tiles) {
-  const long want = (kWanted + groups - 1) / groups, most = (tiles + kAttnWaves - 1) / kAttnWaves;
-  return want < most ? want : most;
+// Wavefronts of a workgroup, and those wanted in a launch: a cache read by few workgroups is cut into pieces.  One block of query rows: 8
+// and two a SIMD (fewer leave loads too few in flight, more pay more prologues and partial results; 4 waves a workgroup / 8, us: 131072
+// rows of 4 KV heads 18.9 / 17.9, 20000 rows of 16 heads, B2 14.0 / 13.1; 8 waves with twice the pieces 19.7, 14.2).  More blocks: 4 and one a
+// SIMD (T5, B4 x 8192 rows, 32 / 8 heads 15.8, twice the pieces 17.7; T12 28.4, 41.4).
+constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
+constexpr long waves_wanted(int nt) { return nt == 1 ? 2048 : 1024; }
+// Up to this many tiles a wave the second launch costs more than the pieces gain (300 rows, 8 KV heads: 6.1 us in one piece, 8.4 in two).
+constexpr long kTilesAlone = 3;
+long splits_for(long groups, long tiles, int nt) {
+  const int waves = waves_of(nt);
+  const long most = (tiles + waves - 1) / waves, least = (tiles + 64 * waves - 1) / (64 * waves);  // one and 64 tiles a wave
+  long want = (waves_wanted(nt) + groups * waves - 1) / (groups * waves);
+  if (most <= kTilesAlone) want = 1;
+  if (want > most) want = most;
+  return want < least ? least : want;
 }
 
 long groups_of(const sa_cache4_desc* c, int T) {
-  const long rows = (long)(c->Hq / c->Hkv) * T, nt = row_tiles(rows);
+  const long rows = (long)(c->Hq / c->Hkv) * T, nt = row_tiles(c, T);
   return (long)c->B * c->Hkv * ((rows + 16 * nt - 1) / (16 * nt));
 }
 
 template <typename T, int D>
-hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, hipStream_t st) {
-  const int nt = row_tiles(a.rows);
+hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, int nt, hipStream_t st) {
   a.row_blocks = (a.rows + 16 * nt - 1) / (16 * nt);
   const long blocks = (long)c->B * c->Hkv * a.row_blocks * a.splits;
   if (blocks > 0x7fffffffL) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
-  if (nt == 1) cache4_attn_kernel<T, D, 1><<<grid, kAttnWaves * 64, 0, st>>>(a);
-  else if (nt == 2) cache4_attn_kernel<T, D, 2><<<grid, kAttnWaves * 64, 0, st>>>(a);
-  else cache4_attn_kernel<T, D, 4><<<grid, kAttnWaves * 64, 0, st>>>(a);
+  const int threads = 64 * waves_of(nt);
+  if (nt == 1) cache4_attn_kernel<T, D, 1, waves_of(1)><<<grid, threads, 0, st>>>(a);
+  else if (nt == 2) cache4_attn_kernel<T, D, 2, waves_of(2)><<<grid, threads, 0, st>>>(a);
+  else if constexpr (sizeof(T) == 2 || D == 64) cache4_attn_kernel<T, D, 4, waves_of(4)><<<grid, threads, 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  cache4_merge_kernel<T, D><<<(unsigned)(c->B * c->Hq * a.T), kMergeWaves * 64, 0, st>>>(a.part, reinterpret_cast<T*>(a.Y), a.LSE, a.splits);
+  const int rows = c->B * c->Hq * a.T;
+  T* Y = reinterpret_cast<T*>(a.Y);
+  if (a.splits <= 16) cache4_merge_kernel<T, D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, Y, a.LSE, a.splits, rows);
+  else cache4_merge_kernel<T, D, 8><<<(unsigned)rows, 512, 0, st>>>(a.part, Y, a.LSE, a.splits, rows);
   return hipGetLastError();
 }
 
@@ -837,7 +859,7 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
   a.c = cache_of(c, pool, table);
   a.starts = starts; a.counts = counts; a.K = K; a.V = V; a.T = T;
   a.tiles = (int)(((long)T + 62) / kTile);  // the first and the last may be begun
-  const long blocks = ((long)c->B * c->Hkv * a.tiles + kRowWaves - 1) / kRowWaves;
+  const long blocks = (long)c->B * c->Hkv * ((a.tiles + kRowWaves - 1) / kRowWaves);
   if (blocks > 0x7fffffffL) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
   const dim3 block(kRowWaves * 64);
@@ -858,7 +880,7 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
 
 size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T) {
   const long tiles = ((long)c->max_pages * c->page_rows) / kTile;
-  const long splits = splits_for(groups_of(c, T), tiles);
+  const long splits = splits_for(groups_of(c, T), tiles, row_tiles(c, T));
   return splits <= 1 ? 0 : (size_t)c->B * c->Hq * T * (size_t)splits * (c->d + 2) * sizeof(float);
 }
 
@@ -869,12 +891,13 @@ hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, c
   a.q = q; a.Y = Y; a.LSE = LSE; a.part = reinterpret_cast<float*>(ws); a.lens = lens;
   a.T = T; a.rows = (c->Hq / c->Hkv) * T; a.max_len = max_len;
   const long tiles = ((long)max_len + kTile - 1) / kTile;
-  const long splits = splits_for(groups_of(c, T), tiles);
+  const int nt = row_tiles(c, T);
+  const long splits = splits_for(groups_of(c, T), tiles, nt);
   a.chunk = (int)((tiles + splits - 1) / splits);
   a.splits = (int)((tiles + a.chunk - 1) / a.chunk);
   a.scale_log2e = (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->d)) * kLog2e;
-  if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, st) : launch_attn<bf16_t, 64>(c, a, st);
-  return c->d == 128 ? launch_attn<float, 128>(c, a, st) : launch_attn<float, 64>(c, a, st);
+  if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, nt, st) : launch_attn<bf16_t, 64>(c, a, nt, st);
+  return c->d == 128 ? launch_attn<float, 128>(c, a, nt, st) : launch_attn<float, 64>(c, a, nt, st);
 }
 
 }  // namespace sa
