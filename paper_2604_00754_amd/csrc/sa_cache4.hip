@@ -76,14 +76,12 @@ struct Elements<bf16_t, E> {
   }
   // largest magnitude as the bits of an fp32 number (an infinity or NaN is above all others)
   __device__ __forceinline__ uint32_t top() const {
-    uint32_t m = 0;
+    typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = {0, 0};
 #pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      const uint32_t lo = (w[i] << 16) & 0x7fffffffu, hi = w[i] & 0x7fff0000u;
-      m = m > lo ? m : lo;
-      m = m > hi ? m : hi;
-    }
-    return m;
+    for (int i = 0; i < E / 2; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    const uint32_t lo = (uint32_t)m[0] << 16, hi = __builtin_bit_cast(uint32_t, m) & 0xffff0000u;
+    return lo > hi ? lo : hi;
   }
   __device__ __forceinline__ uint32_t codes(float scale) const {
     uint32_t c = 0;
@@ -145,32 +143,32 @@ struct RowsArgs {
   int T, tiles;  // tiles a sequence's rows can touch
 };
 
-// What a wave of the two row kernels works on: the rows t0 + row(g, j) of one sequence and head that lie in one tile.
+// What a wave of the two row kernels works on: a half of 16 rows of a tile, 4 a lane group, K and V of a row by the same lanes.
 struct Rows {
-  int b, hk, tile;  // tile: -1 outside the sequence's positions
-  long t0;          // t of the tile's first row
+  int b, hk, tile, half;  // tile: -1 outside the sequence's positions
+  long t0;                // t of the half's first row
   int count;
-  bool any, whole;  // whether rows of the tile are among them, and all
+  bool any, whole;        // whether rows of the half are among those asked for, and all
 };
 constexpr int kRowWaves = 4;
 __device__ __forceinline__ Rows rows_of_wave(const RowsArgs& a) {
   Rows w;
-  const unsigned blocks = (unsigned)(a.tiles + kRowWaves - 1) / kRowWaves, bh = blockIdx.x / blocks;
+  const unsigned blocks = (unsigned)(2 * a.tiles + kRowWaves - 1) / kRowWaves, bh = blockIdx.x / blocks;
   const int k = (int)(blockIdx.x % blocks) * kRowWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   w.hk = (int)(bh % (unsigned)a.c.Hkv);
   w.b = (int)(bh / (unsigned)a.c.Hkv);
+  w.half = k & 1;
   const int start = a.starts ? __builtin_amdgcn_readfirstlane(a.starts[w.b]) : 0;
   w.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[w.b], 0), a.T)) : a.T;
-  const long tile = (long)(start >> 5) + k;
-  w.t0 = tile * kTile - start;
-  w.any = k < a.tiles && w.t0 < w.count;
-  w.whole = w.t0 >= 0 && w.t0 + kTile <= w.count;
+  const long tile = (long)(start >> 5) + (k >> 1);
+  w.t0 = tile * kTile + 16 * w.half - start;
+  w.any = k < 2 * a.tiles && w.t0 < w.count && w.t0 + 16 > 0;
+  w.whole = w.t0 >= 0 && w.t0 + 16 <= w.count;
   w.tile = tile < 0 || tile * kTile >= a.c.capacity ? -1 : (int)tile;
   return w;
 }
 
-// One wave per tile that the rows touch, 8 rows a lane group, K and V of a row by the same lanes: a row that holds an infinity or
-// NaN in either is marked in both.  Bound: HBM (reads 4 d bytes a row in bf16, writes 17/16 d).
+// A row that holds an infinity or NaN in K or V is marked in both.  Bound: HBM (reads 4 d bytes a row in bf16, writes 17/16 d).
 template <typename T, int D>
 __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a) {
   using L = Tile<D>;
@@ -182,22 +180,22 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4;
   unsigned char* base = a.c.pool + (size_t)number * L::kBytes;
   const size_t src = ((size_t)w.b * a.c.Hkv + w.hk) * a.T;
-  Elements<T, E> k[8], v[8];
-  bool in[8];
+  Elements<T, E> k[4], v[4];
+  bool in[4];
   const T* kr = reinterpret_cast<const T*>(a.K) + src * D + r * E;
   const T* vr = reinterpret_cast<const T*>(a.V) + src * D + r * E;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {  // (rows of the tile that are not written: the first or last that is in their place)
-    const long t = w.t0 + L::row(g, j);
+  for (int j = 0; j < 4; ++j) {  // (rows that are not written: the first or last that is in their place)
+    const long t = w.t0 + 4 * g + j;
     in[j] = t >= 0 && t < w.count;
     const size_t at = (size_t)(t < 0 ? 0 : t < w.count ? t : w.count - 1) * D;
     k[j].load(kr + at);
     v[j].load(vr + at);
   }
   __builtin_amdgcn_sched_barrier(0);  // all loads in flight together
-  uint32_t kc[8], vc[8], ks[8], vs[8];
+  uint32_t kc[4], vc[4], ks[4], vs[4];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
+  for (int j = 0; j < 4; ++j) {
     const uint32_t kt = block_max<L::LPB>(k[j].top()), vt = block_max<L::LPB>(v[j].top());
     const bool bad = row_max<L::LPB>(kt > vt ? kt : vt) >= 0x7f800000u;
     ks[j] = scale_byte(kt);
@@ -209,43 +207,32 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
     ks[j] = bad ? kNoRow : ks[j];
     vs[j] = bad ? kOne : vs[j];
   }
-  // K codes: rows as they are; V codes: the 8 rows of a lane group side by side; scales: by the first lane of a block
-  unsigned char* kp = base + (4 * g) * (D / 2) + r * L::RB;
-  unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
+  // K codes: rows as they are; V codes: the 4 rows of a lane group side by side; scales: by the first lane of a block
+  unsigned char* kp = base + (16 * w.half + 4 * g) * (D / 2) + r * L::RB;
+  unsigned char* vp = base + L::kV + ((g * 16 + r) * 2 + w.half) * 4 * L::RB;
   const int c = r / L::LPB;
-  unsigned char* kq = base + L::kKs + (c * 16 + 4 * g) * 2;
-  unsigned char* vq = base + L::kVs + (c * 4 + g) * 8;
+  unsigned char* kq = base + L::kKs + (c * 16 + 4 * g) * 2 + w.half;
+  unsigned char* vq = base + L::kVs + ((c * 4 + g) * 2 + w.half) * 4;
   const auto put_k = [&](int j) {
-    unsigned char* to = kp + L::row(0, j) * (D / 2);
-    if constexpr (L::RB == 4) *reinterpret_cast<uint32_t*>(to) = kc[j];
-    else *reinterpret_cast<uint16_t*>(to) = (uint16_t)kc[j];
+    if constexpr (L::RB == 4) *reinterpret_cast<uint32_t*>(kp + j * (D / 2)) = kc[j];
+    else *reinterpret_cast<uint16_t*>(kp + j * (D / 2)) = (uint16_t)kc[j];
+    if (r % L::LPB == 0) kq[2 * j] = (unsigned char)ks[j];
   };
   if (w.whole) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) put_k(j);
-    if constexpr (L::RB == 4) {
-      reinterpret_cast<u32x4*>(vp)[0] = u32x4{vc[0], vc[1], vc[2], vc[3]};
-      reinterpret_cast<u32x4*>(vp)[1] = u32x4{vc[4], vc[5], vc[6], vc[7]};
-    } else {
-      *reinterpret_cast<u32x4*>(vp) = u32x4{(vc[0] & 0xffffu) | (vc[1] << 16), (vc[2] & 0xffffu) | (vc[3] << 16),
-                                            (vc[4] & 0xffffu) | (vc[5] << 16), (vc[6] & 0xffffu) | (vc[7] << 16)};
-    }
-    if (r % L::LPB == 0) {
-      *reinterpret_cast<u32x2*>(kq) = u32x2{ks[0] | ks[4] << 8 | ks[1] << 16 | ks[5] << 24, ks[2] | ks[6] << 8 | ks[3] << 16 | ks[7] << 24};
-      *reinterpret_cast<u32x2*>(vq) = u32x2{vs[0] | vs[1] << 8 | vs[2] << 16 | vs[3] << 24, vs[4] | vs[5] << 8 | vs[6] << 16 | vs[7] << 24};
-    }
+    for (int j = 0; j < 4; ++j) put_k(j);
+    if constexpr (L::RB == 4) *reinterpret_cast<u32x4*>(vp) = u32x4{vc[0], vc[1], vc[2], vc[3]};
+    else *reinterpret_cast<u32x2*>(vp) = u32x2{(vc[0] & 0xffffu) | (vc[1] << 16), (vc[2] & 0xffffu) | (vc[3] << 16)};
+    if (r % L::LPB == 0) *reinterpret_cast<uint32_t*>(vq) = vs[0] | vs[1] << 8 | vs[2] << 16 | vs[3] << 24;
     return;
   }
 #pragma unroll
-  for (int j = 0; j < 8; ++j)
+  for (int j = 0; j < 4; ++j)
     if (in[j]) {
       put_k(j);
       if constexpr (L::RB == 4) reinterpret_cast<uint32_t*>(vp)[j] = vc[j];
       else reinterpret_cast<uint16_t*>(vp)[j] = (uint16_t)vc[j];
-      if (r % L::LPB == 0) {
-        kq[2 * (j & 3) + (j >> 2)] = (unsigned char)ks[j];
-        vq[j] = (unsigned char)vs[j];
-      }
+      if (r % L::LPB == 0) vq[j] = (unsigned char)vs[j];
     }
 }
 
@@ -299,33 +286,33 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a)
   const bool there = number >= 0;
   const int lane = threadIdx.x & 63, r = lane & 15, g = lane >> 4, c = r / L::LPB;
   const unsigned char* base = a.c.pool + (size_t)(there ? number : 0) * L::kBytes;
-  uint32_t kc[8] = {}, vc[8] = {};
-  u32x2 ks = {}, vs = {};
+  uint32_t kc[4] = {}, vc[4] = {}, vs = 0;
+  u32x2 ks = {};  // of both halves
   if (there) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const unsigned char* kp = base + L::row(g, j) * (D / 2) + r * L::RB;
+    for (int j = 0; j < 4; ++j) {
+      const unsigned char* kp = base + (16 * w.half + 4 * g + j) * (D / 2) + r * L::RB;
       if constexpr (L::RB == 4) kc[j] = *reinterpret_cast<const uint32_t*>(kp);
       else kc[j] = *reinterpret_cast<const uint16_t*>(kp);
     }
-    const unsigned char* vp = base + L::kV + (g * 16 + r) * 8 * L::RB;
-    const u32x4 x = reinterpret_cast<const u32x4*>(vp)[0];
+    const unsigned char* vp = base + L::kV + ((g * 16 + r) * 2 + w.half) * 4 * L::RB;
     if constexpr (L::RB == 4) {
-      const u32x4 y = reinterpret_cast<const u32x4*>(vp)[1];
+      const u32x4 x = *reinterpret_cast<const u32x4*>(vp);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) { vc[j] = x[j]; vc[4 + j] = y[j]; }
+      for (int j = 0; j < 4; ++j) vc[j] = x[j];
     } else {
+      const u32x2 x = *reinterpret_cast<const u32x2*>(vp);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vc[j] = (x[j / 2] >> (16 * (j & 1))) & 0xffffu;
+      for (int j = 0; j < 4; ++j) vc[j] = (x[j / 2] >> (16 * (j & 1))) & 0xffffu;
     }
     ks = *reinterpret_cast<const u32x2*>(base + L::kKs + (c * 16 + 4 * g) * 2);
-    vs = *reinterpret_cast<const u32x2*>(base + L::kVs + (c * 4 + g) * 8);
+    vs = *reinterpret_cast<const uint32_t*>(base + L::kVs + ((c * 4 + g) * 2 + w.half) * 4);
   }
   const size_t dst = ((size_t)w.b * a.c.Hkv + w.hk) * a.T;
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    const long t = w.t0 + L::row(g, j);
-    const uint32_t kb = (ks[(j & 3) / 2] >> (16 * (j & 1) + 8 * (j >> 2))) & 0xffu, vb = (vs[j / 4] >> (8 * (j & 3))) & 0xffu;
+  for (int j = 0; j < 4; ++j) {
+    const long t = w.t0 + 4 * g + j;
+    const uint32_t kb = (ks[j / 2] >> (16 * (j & 1) + 8 * w.half)) & 0xffu, vb = (vs >> (8 * j)) & 0xffu;
     if (t >= 0 && t < w.count) {
       const size_t at = (dst + (size_t)t) * D + r * L::E;
       const bool nan = kb == kNoRow;
@@ -859,7 +846,7 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
   a.c = cache_of(c, pool, table);
   a.starts = starts; a.counts = counts; a.K = K; a.V = V; a.T = T;
   a.tiles = (int)(((long)T + 62) / kTile);  // the first and the last may be begun
-  const long blocks = (long)c->B * c->Hkv * ((a.tiles + kRowWaves - 1) / kRowWaves);
+  const long blocks = (long)c->B * c->Hkv * ((2 * (long)a.tiles + kRowWaves - 1) / kRowWaves);
   if (blocks > 0x7fffffffL) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
   const dim3 block(kRowWaves * 64);
