@@ -116,6 +116,8 @@ def _load():
     lib.sa_internal_bwd_kernel.argtypes = [dp, C.c_int, C.c_int]
     lib.sa_internal_gate_kernel.restype = C.c_char_p
     lib.sa_internal_gate_kernel.argtypes = [dp, C.c_int, C.c_int]
+    lib.sa_internal_cache4_plan.restype = C.c_int
+    lib.sa_internal_cache4_plan.argtypes = [cp, C.c_int, C.c_int]
     lib.sa_internal_gate_dw_pieces.restype = C.c_int
     lib.sa_internal_gate_dw_pieces.argtypes = [dp, C.c_int]
     lib.swa_fwd.restype = C.c_int
@@ -347,6 +349,12 @@ def gate_kernel(desc, backward=False, dual=True) -> str:
 def gate_dw_pieces(desc, dual=True) -> int:
     """Pieces of the tokens that sa_gate_proj_bwd adds up to a tile of dW."""
     return _lib.sa_internal_gate_dw_pieces(C.byref(desc), int(dual))
+
+
+def cache4_plan(desc, T, max_len):
+    """How sa_cache4_decode_fwd deals a call: (blocks of 16 query rows a wave takes, pieces of the cache)."""
+    p = _lib.sa_internal_cache4_plan(C.byref(desc), int(T), int(max_len))
+    return p & 3, p >> 2
 
 
 def raw():

@@ -347,7 +347,8 @@ struct AttnArgs {
 
 // The maximum is raised where a score passes it by more than this; the largest probability is then 2^15, with the lift, and the smallest
 // that f16 holds to all its bits 2^-21 of the largest possible.
-constexpr float kRaise = 8.f, kLift = 7.f;
+// kNone: the maximum before a row has been seen, a finite number (a row that is not seen has the score -inf).
+constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.0e38f;
 
 __device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
 
@@ -384,7 +385,7 @@ __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __bu
 typedef __amdgpu_buffer_rsrc_t tile_buffer;
 template <int D>
 struct TileRegs {
-  uint32_t k[2][D / 32];  // [half][word]: 8 elements a word
+  uint32_t k[2][D / 32];  // [half][word], 8 elements a word: D/4 of them from D/4 g on (D = 128: the block of 32 elements g)
   uint32_t v[D / 16];     // D = 128: a word per row j; D = 64: rows 2j, 2j + 1 share one
   uint32_t ks;            // scale bytes of the halves
   u32x2 vs;               // of rows j
@@ -436,25 +437,29 @@ __device__ __forceinline__ bf16x8 eight_values(uint32_t codes, float scale) {
   return __builtin_bit_cast(bf16x8, w);
 }
 
+// The probabilities of 8 rows as the operand's PARTS
+template <typename V, int PARTS>
+__device__ __forceinline__ void pack_weights(const float* p, V (&pf)[PARTS]) {
+  u32x4 w[PARTS];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t parts[PARTS];
+    if constexpr (__is_same(V, bf16x8)) split_pair_bf16<PARTS>(p[2 * i], p[2 * i + 1], parts);
+    else split_pair_f16<PARTS>(p[2 * i], p[2 * i + 1], parts);
+#pragma unroll
+    for (int k = 0; k < PARTS; ++k) w[k][i] = parts[k];
+  }
+#pragma unroll
+  for (int k = 0; k < PARTS; ++k) pf[k] = __builtin_bit_cast(V, w[k]);
+}
+
 // O^T += V^T P^T over the 8 rows of each lane group, for every block of query rows.  V is the operand type: f16 with P in PARTS of 11
 // bits, or bf16 with parts of 8 where a scale of the tile is out of f16's reach.  p: the probabilities, rows 4 half + i.
 template <typename V, int D, int NT, int PARTS>
 __device__ __forceinline__ void add_pv(const uint32_t* v, const float* vscale, const float (*p)[8], f32x4 (*o)[D / 16]) {
   V pf[NT][PARTS];
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    u32x4 w[PARTS];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      uint32_t parts[PARTS];
-      if constexpr (__is_same(V, bf16x8)) split_pair_bf16<PARTS>(p[n][2 * i], p[n][2 * i + 1], parts);
-      else split_pair_f16<PARTS>(p[n][2 * i], p[n][2 * i + 1], parts);
-#pragma unroll
-      for (int k = 0; k < PARTS; ++k) w[k][i] = parts[k];
-    }
-#pragma unroll
-    for (int k = 0; k < PARTS; ++k) pf[n][k] = __builtin_bit_cast(V, w[k]);
-  }
+  for (int n = 0; n < NT; ++n) pack_weights<V, PARTS>(p[n], pf[n]);
 #pragma unroll
   for (int q = 0; q < D / 32; ++q) {
     uint32_t pr[8];
@@ -494,8 +499,65 @@ __device__ __forceinline__ void load_q8<float>(const float* p, float (&x)[8]) {
 __device__ __forceinline__ void store_y(bf16_t* p, float v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
 __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 
+// The lane's part of its query rows (past the last: that one again) as operands
+template <typename T, int D, int NT, int QP>
+__device__ __forceinline__ void load_queries(const T* q, int row0, int rows, int r, int g, bf16x8 (&qf)[NT][D / 32][QP]) {
+#pragma unroll
+  for (int n = 0; n < NT; ++n) {
+    const int c = min(row0 + 16 * n + r, rows - 1);
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) {
+      float x[8];
+      load_q8<T>(q + (size_t)c * D + (D / 4) * g + 8 * s, x);
+      u32x4 w[QP];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        uint32_t p[QP];
+        split_pair_bf16<QP>(x[2 * i], x[2 * i + 1], p);
+#pragma unroll
+        for (int k = 0; k < QP; ++k) w[k][i] = p[k];
+      }
+#pragma unroll
+      for (int k = 0; k < QP; ++k) qf[n][s][k] = __builtin_bit_cast(bf16x8, w[k]);
+    }
+  }
+}
+
+// Scores of 8 rows -> probabilities relative to the running maximum m (log2 domain, 2^kLift above it), their sum added to l.  They are
+// formed with the maximum at hand; where one is past 2^(kLift + kRaise), the maximum is raised and l and o are brought to the new one.
+template <int D>
+__device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, float& l, f32x4* o) {
+  float e[8], ref = kLift - m;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) e[j] = fmaf(p[j], scale_log2e, ref);
+  float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), e[2]), fmaxf(fmaxf(e[3], e[4]), e[5]));
+  top = fmaxf(fmaxf(top, e[6]), e[7]);
+  if (__any(top > kLift + kRaise)) {
+    float mn = p[0];
+#pragma unroll
+    for (int j = 1; j < 8; ++j) mn = fmaxf(mn, p[j]);
+    mn = fmaxf(mn, __shfl_xor(mn, 16));
+    mn = fmaxf(m, fmaxf(mn, __shfl_xor(mn, 32)) * scale_log2e);
+    const float corr = exp2f(m - mn);
+    l *= corr;
+#pragma unroll
+    for (int d = 0; d < D / 16; ++d) o[d] *= corr;
+    m = mn;
+    ref = kLift - m;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = fmaf(p[j], scale_log2e, ref);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    p[j] = __builtin_amdgcn_exp2f(e[j]);
+    l += p[j];
+  }
+}
+
+// Lists of 64 tiles that a wave keeps the numbers of.
+constexpr int lists_of(int nt) { return nt == 1 ? 1 : 2; }
 // Wavefronts a SIMD that the registers are kept for: what the compiler reaches without spilling.
-constexpr int attn_waves_per_simd(bool bf16, int D, int NT) { return NT == 1 ? (bf16 ? 4 : 3) : NT == 2 ? (D == 64 ? 3 : 2) : D == 64 && bf16 ? 2 : 1; }
+constexpr int attn_waves_per_simd(bool bf16, int D, int NT) { return NT == 1 ? (bf16 ? 4 : 3) : D == 64 ? 3 : 2; }
 
 template <typename T, int D, int NT, int W>
 __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT)) void cache4_attn_kernel(AttnArgs a) {
@@ -505,6 +567,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
   constexpr int KS = D / 32;                   // steps of the score product
   constexpr int DB = D / 16;                   // blocks of 16 elements
   constexpr int LD = D + 4;                    // floats between rows of the merge area
+  constexpr int kLists = lists_of(NT);
   __shared__ __align__(16) float lds_o[W][16][LD];
   __shared__ float lds_ml[W][16][2];
 
@@ -515,10 +578,21 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
   const int bh = (int)(rest / (unsigned)a.row_blocks);
   const int hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
   const int row0 = rb * 16 * NT;
-  // The numbers of the wave's tiles (64 at most), one a lane: of every tile that the longest sequence could have, so that the page
+  // The numbers of the wave's tiles (64 kLists at most), one a lane: of every tile that the longest sequence could have, so that the page
   // table's entries arrive together with the sequence's length and not behind it.
   const int first = split * a.chunk + wave, end = min((split + 1) * a.chunk, (a.max_len + kTile - 1) / kTile);
-  const int numbers = first + W * lane < end ? tile_number(a.c, b, hk, first + W * lane) : -1;
+  int numbers[kLists];
+#pragma unroll
+  for (int k = 0; k < kLists; ++k) {
+    const int tile = first + W * (64 * k + lane);
+    numbers[k] = tile < end ? tile_number(a.c, b, hk, tile) : -1;
+  }
+  const auto number_of = [&](int i) {
+    int n = __builtin_amdgcn_readlane(numbers[0], i & 63);
+#pragma unroll
+    for (int k = 1; k < kLists; ++k) n = i >> 6 == k ? __builtin_amdgcn_readlane(numbers[k], i & 63) : n;
+    return n;
+  };
   const int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[b], 0), a.max_len));
 
   // the last position each of the lane's query rows sees (-1 or less: none), and their largest and smallest over the block
@@ -534,25 +608,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
 
   const T* qrows = reinterpret_cast<const T*>(a.q) + (size_t)bh * a.rows * D;
   bf16x8 qf[NT][KS][QP];
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int c = min(row0 + 16 * n + r, a.rows - 1);
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      float x[8];
-      load_q8<T>(qrows + (size_t)c * D + (D / 4) * g + 8 * s, x);
-      u32x4 w[QP];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        uint32_t p[QP];
-        split_pair_bf16<QP>(x[2 * i], x[2 * i + 1], p);
-#pragma unroll
-        for (int k = 0; k < QP; ++k) w[k][i] = p[k];
-      }
-#pragma unroll
-      for (int k = 0; k < QP; ++k) qf[n][s][k] = __builtin_bit_cast(bf16x8, w[k]);
-    }
-  }
+  load_queries<T, D, NT>(qrows, row0, a.rows, r, g, qf);
 
   f32x4 o[NT][DB];
   float m[NT], l[NT];
@@ -566,12 +622,12 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     for (int n = 0; n < NT; ++n) {
 #pragma unroll
       for (int d = 0; d < DB; ++d) o[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
-      m[n] = -INFINITY;
+      m[n] = kNone;
       l[n] = 0.f;
     }
     TileRegs<D> x;
     auto place = [&](int i) {  // (a tile that is not there: the first of the pool in its place, not seen)
-      const int number = __builtin_amdgcn_readlane(numbers, i);
+      const int number = number_of(i);
       return __builtin_amdgcn_make_buffer_rsrc(a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes, 0, L::kBytes, 0x20000);
     };
     x.place(r, g);
@@ -581,7 +637,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     x.load_v(place(0));
     __builtin_amdgcn_sched_barrier(0);
     for (int i = 0; i < turns; ++i) {
-      const bool there = __builtin_amdgcn_readlane(numbers, i) >= 0;
+      const bool there = number_of(i) >= 0;
       const tile_buffer next = place(min(i + 1, turns - 1));  // (the last turn asks for its own again: the loads need no branch)
       const int tile = first + W * i;
       const bool partly = tile * kTile + kTile - 1 > least || !there;  // some query row does not see all of it
@@ -623,25 +679,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
         unfit |= off & 0xe0e0e0e0u;
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float top = fmaxf(fmaxf(fmaxf(p[n][0], p[n][1]), fmaxf(p[n][2], p[n][3])), fmaxf(fmaxf(p[n][4], p[n][5]), fmaxf(p[n][6], p[n][7])));
-        top *= a.scale_log2e;
-        if (__any(top > m[n] + kRaise)) {   // (m = -inf at first)
-          float mn = fmaxf(top, __shfl_xor(top, 16));
-          mn = fmaxf(m[n], fmaxf(mn, __shfl_xor(mn, 32)));
-          const float corr = exp2_above(m[n], mn);
-          l[n] *= corr;
-#pragma unroll
-          for (int d = 0; d < DB; ++d) o[n][d] *= corr;
-          m[n] = mn;
-        }
-        const float ref = m[n] == -INFINITY ? 0.f : kLift - m[n];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[n][j] = __builtin_amdgcn_exp2f(fmaf(p[n][j], a.scale_log2e, ref));
-          l[n] += p[n][j];
-        }
-      }
+      for (int n = 0; n < NT; ++n) weigh<D>(p[n], a.scale_log2e, m[n], l[n], o[n]);
       __builtin_amdgcn_sched_barrier(0);
       float vscale[8];
 #pragma unroll
@@ -791,44 +829,56 @@ Cache cache_of(const sa_cache4_desc* c, void* pool, const int32_t* table) {
   return k;
 }
 
-// Blocks of 16 query rows a wave takes (fp32 rows of 128 at most two: four spill).
-int row_tiles(const sa_cache4_desc* c, int T) {
-  const long rows = (long)(c->Hq / c->Hkv) * T;
-  return rows <= 16 ? 1 : rows <= 32 || (c->dtype == SA_F32 && c->d == 128) ? 2 : 4;
-}
-
-// Wavefronts of a workgroup, and those wanted in a launch: a cache read by few workgroups is cut into pieces.  One block of query rows: 8
-// and two a SIMD (fewer leave loads too few in flight, more pay more prologues and partial results; 4 waves a workgroup / 8, us: 131072
-// rows of 4 KV heads 18.9 / 17.9, 20000 rows of 16 heads, B2 14.0 / 13.1; 8 waves with twice the pieces 19.7, 14.2).  More blocks: 4 and one a
-// SIMD (T5, B4 x 8192 rows, 32 / 8 heads 15.8, twice the pieces 17.7; T12 28.4, 41.4).
+// How a call is dealt: the query rows of a KV head in `blocks` of 16 nt, the cache in `splits` pieces; `most`: what `splits` can be
+// for this many tiles or fewer (the workspace is sized for that).
+struct Plan {
+  int nt;
+  long blocks, splits, most;
+};
 constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
-constexpr long waves_wanted(int nt) { return nt == 1 ? 2048 : 1024; }
-// Up to this many tiles a wave the second launch costs more than the pieces gain (300 rows, 8 KV heads: 6.1 us in one piece, 8.4 in two).
-constexpr long kTilesAlone = 3;
-long splits_for(long groups, long tiles, int nt) {
-  const int waves = waves_of(nt);
-  const long most = (tiles + waves - 1) / waves, least = (tiles + 64 * waves - 1) / (64 * waves);  // one and 64 tiles a wave
-  long want = (waves_wanted(nt) + groups * waves - 1) / (groups * waves);
-  if (most <= kTilesAlone) want = 1;
-  if (want > most) want = most;
-  return want < least ? least : want;
-}
-
-long groups_of(const sa_cache4_desc* c, int T) {
-  const long rows = (long)(c->Hq / c->Hkv) * T, nt = row_tiles(c, T);
-  return (long)c->B * c->Hkv * ((rows + 16 * nt - 1) / (16 * nt));
+Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
+  const long rows = (long)(c->Hq / c->Hkv) * T;
+  Plan p;
+  p.nt = rows <= 16 ? 1 : 2;
+  p.blocks = (rows + 16 * p.nt - 1) / (16 * p.nt);
+  const long groups = (long)c->B * c->Hkv * p.blocks;
+  const long waves = waves_of(p.nt), whole = 64 * lists_of(p.nt) * waves;
+  const long least = (tiles + whole - 1) / whole, all = (tiles + waves - 1) / waves;  // as many tiles a wave as it can list, and one
+  const auto between = [&](long want) { return want > all ? (all < least ? least : all) : want < least ? least : want; };
+  if (p.nt == 1) {
+    // Bound by memory: two waves a SIMD.  Fewer leave loads too few in flight, more pay more prologues and partial results (us, workgroups of 4
+    // waves / 8 / 8 with twice the pieces: 131072 rows of 4 KV heads 18.9 / 17.9 / 19.7, 20000 rows of 16 heads, B2 14.0 / 13.1 / 14.2).
+    // Up to three tiles a wave the second launch costs more than pieces gain (300 rows, 8 KV heads: 6.1 us in one piece, 8.4 in two).
+    p.splits = p.most = all <= 3 ? between(1) : between((2048 + groups * waves - 1) / (groups * waves));
+    return p;
+  }
+  // Bound by the vector ALU.  The launch is as many workgroups at a time as fit the chip, each a piece's tiles long and what a prologue and an
+  // end take, about six; with k waves a SIMD all of that takes 1 + 0.6 (k - 1) times as long as with one; joining pieces takes about
+  // eight.  The least of that for pieces that fill one, two, .. waves a SIMD, and two and three such rounds (us, pieces of one / two waves:
+  // T5, B4 x 8192 rows, 32 / 8 heads 15.4 / 17.7; T128 over 32768 rows 95 / 79; T509 over 32768 rows in two and a part rounds 295, in two 275).
+  const int per_simd = attn_waves_per_simd(c->dtype == SA_BF16, c->d, p.nt);
+  const long fit = 256 * per_simd;  // (a workgroup is a wave on each SIMD)
+  p.splits = least;
+  p.most = between(3 * fit / groups + 1);
+  long best = 0;
+  for (int k = 0; k <= per_simd + 2; ++k) {
+    const long room = (k <= per_simd ? 256 * k : fit * (k - per_simd + 1)) / groups;
+    const long s = room < least ? least : room > p.most ? p.most : room;
+    const long rounds = (groups * s + fit - 1) / fit, each = (tiles + s * waves - 1) / (s * waves) + 6;
+    const long shared = ((groups * s < fit ? groups * s : fit) + 255) / 256;
+    const long cost = rounds * each * (4 + 6 * shared) + (s > 1 ? 80 : 0);  // in tenths
+    if (best == 0 || cost < best) { best = cost; p.splits = s; }
+  }
+  return p;
 }
 
 template <typename T, int D>
-hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, int nt, hipStream_t st) {
-  a.row_blocks = (a.rows + 16 * nt - 1) / (16 * nt);
+hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, const Plan& p, hipStream_t st) {
   const long blocks = (long)c->B * c->Hkv * a.row_blocks * a.splits;
   if (blocks > 0x7fffffffL) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
-  const int threads = 64 * waves_of(nt);
-  if (nt == 1) cache4_attn_kernel<T, D, 1, waves_of(1)><<<grid, threads, 0, st>>>(a);
-  else if (nt == 2) cache4_attn_kernel<T, D, 2, waves_of(2)><<<grid, threads, 0, st>>>(a);
-  else if constexpr (sizeof(T) == 2 || D == 64) cache4_attn_kernel<T, D, 4, waves_of(4)><<<grid, threads, 0, st>>>(a);
+  if (p.nt == 1) cache4_attn_kernel<T, D, 1, waves_of(1)><<<grid, 64 * waves_of(1), 0, st>>>(a);
+  else cache4_attn_kernel<T, D, 2, waves_of(2)><<<grid, 64 * waves_of(2), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
   const int rows = c->B * c->Hq * a.T;
@@ -867,8 +917,13 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
 
 size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T) {
   const long tiles = ((long)c->max_pages * c->page_rows) / kTile;
-  const long splits = splits_for(groups_of(c, T), tiles, row_tiles(c, T));
+  const long splits = plan_of(c, T, tiles).most;
   return splits <= 1 ? 0 : (size_t)c->B * c->Hq * T * (size_t)splits * (c->d + 2) * sizeof(float);
+}
+
+int cache4_decode_plan(const sa_cache4_desc* c, int T, int max_len) {
+  const Plan p = plan_of(c, T, ((long)max_len + kTile - 1) / kTile);
+  return p.nt | (int)p.splits << 2;
 }
 
 hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, const void* pool, const int32_t* table,
@@ -878,13 +933,13 @@ hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, c
   a.q = q; a.Y = Y; a.LSE = LSE; a.part = reinterpret_cast<float*>(ws); a.lens = lens;
   a.T = T; a.rows = (c->Hq / c->Hkv) * T; a.max_len = max_len;
   const long tiles = ((long)max_len + kTile - 1) / kTile;
-  const int nt = row_tiles(c, T);
-  const long splits = splits_for(groups_of(c, T), tiles, nt);
-  a.chunk = (int)((tiles + splits - 1) / splits);
+  const Plan p = plan_of(c, T, tiles);
+  a.row_blocks = (int)p.blocks;
+  a.chunk = (int)((tiles + p.splits - 1) / p.splits);
   a.splits = (int)((tiles + a.chunk - 1) / a.chunk);
   a.scale_log2e = (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->d)) * kLog2e;
-  if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, nt, st) : launch_attn<bf16_t, 64>(c, a, nt, st);
-  return c->d == 128 ? launch_attn<float, 128>(c, a, nt, st) : launch_attn<float, 64>(c, a, nt, st);
+  if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, p, st) : launch_attn<bf16_t, 64>(c, a, p, st);
+  return c->d == 128 ? launch_attn<float, 128>(c, a, p, st) : launch_attn<float, 64>(c, a, p, st);
 }
 
 }  // namespace sa

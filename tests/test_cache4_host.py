@@ -136,6 +136,38 @@ def test_workspaces():
     assert sa.sa_cache4_workspace_bytes(d, 99, 1) == 0
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,d,dtype,T,n,kernel,pieces", [
+    (1, 32, 8, 128, 0, 1, 300, 1, 1),          # three tiles a wave at most: one launch
+    (1, 32, 8, 128, 0, 1, 1100, 1, 5),         # a tile a wave
+    (1, 32, 4, 128, 0, 1, 131072, 1, 64),      # two waves a SIMD
+    (16, 32, 8, 128, 0, 1, 8192, 1, 2),
+    (64, 16, 16, 64, 0, 1, 131072, 1, 8),      # 64 tiles a wave and no more
+    (4, 32, 8, 128, 0, 5, 8192, 2, 8),         # one wave a SIMD
+    (1, 32, 8, 128, 0, 64, 32768, 2, 8),       # two
+    (1, 32, 8, 128, 0, 509, 32768, 2, 2),      # two whole rounds
+    (1, 32, 8, 128, 1, 509, 32768, 2, 2),
+    (1, 16, 16, 64, 0, 512, 512, 2, 1),
+    (1, 2, 1, 128, 0, 2000, 1 << 20, 2, 64),   # 128 tiles a wave and no more
+])
+def test_how_attention_is_dealt(B, Hq, Hkv, d, dtype, T, n, kernel, pieces):
+    c = desc(B=B, Hq=Hq, Hkv=Hkv, d=d, dtype=dtype, max_pages=-(-n // 64), pages=100)
+    assert sa.cache4_plan(c, T, n) == (kernel, pieces)
+
+
+def test_workspaces_cover_every_length():
+    rng = np.random.default_rng(0)
+    for _ in range(300):
+        Hkv, g, M = int(rng.integers(1, 9)), int(rng.integers(1, 9)), int(np.exp(rng.uniform(0, 8)))
+        c = desc(B=int(rng.integers(1, 20)), Hq=Hkv * g, Hkv=Hkv, d=int(rng.choice([64, 128])), dtype=int(rng.integers(0, 2)), max_pages=M, pages=9)
+        T = int(np.exp(rng.uniform(0, 6)))
+        need = sa.sa_cache4_workspace_bytes(c, sa.SA_OP_CACHE4_DECODE, T)
+        for n in {1, 64 * M, *np.exp(rng.uniform(0, np.log(64 * M), 20)).astype(int).tolist()}:
+            kernel, pieces = sa.cache4_plan(c, T, n)
+            tiles, waves = -(-n // 32), 8 if kernel == 1 else 4
+            assert pieces <= -(-tiles // waves) and -(-tiles // pieces) <= waves * (64 if kernel == 1 else 128)
+            assert pieces == 1 or need >= c.B * c.Hq * T * pieces * (c.d + 2) * 4
+
+
 def test_outputs_that_overlap_inputs():
     d = desc()
     name = "sa_pages_fork"

@@ -262,6 +262,67 @@ def test_values_of_any_size(dtype, d, sizes):
     c.check(20, [250])
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,d,dtype,T,lens,kernel", [
+    (1, 8, 2, 128, "bf16", 300, [6500], 2),         # pieces
+    (1, 32, 8, 128, "bf16", 200, [5000], 2),        # more workgroups than fit
+    (2, 8, 2, 128, "bf16", 511, [9001, 300], 2),    # a sequence shorter than its tokens, which see rows in part or none
+    (1, 8, 2, 64, "bf16", 300, [6500], 2),
+    (1, 8, 2, 128, "f32", 300, [6500], 2),
+    (1, 8, 1, 64, "f32", 65, [20011], 2),
+    (1, 32, 4, 128, "bf16", 1, [40001], 1),
+    (3, 12, 12, 64, "bf16", 1, [30000, 1, 777], 1),
+])
+def test_many_rows(B, Hq, Hkv, d, dtype, T, lens, kernel):
+    """Long caches and many tokens against fp64 on the rows as they are read back; some elements of q 60 times as large as others, some a
+    millionth"""
+    n = max(lens)
+    c = Setup(B, Hq, Hkv, d, 64, -(-n // 64), dtype, seed=T + d)
+    assert sa().cache4_plan(c.desc, T, n)[0] == kernel
+    g = torch.Generator(device=U.DEV).manual_seed(T)
+    K, V = (torch.randn(B, Hkv, n, d, device=U.DEV, generator=g).to(U.tdtype(dtype)) for _ in "KV")
+    table = c.dev(c.table)
+    sa().sa_cache4_write(c.desc, K, V, None, c.dev(np.array(lens, np.int32)), table, c.pool)
+    sa().sa_cache4_read(c.desc, c.pool, table, None, None, K, V)
+    q = torch.randn(B, Hq, T, d, device=U.DEV, generator=g)
+    q[..., 5] *= 60
+    q[..., 37] *= 1e-6
+    q, Y, L = c.decode(T, lens, q=q.to(U.tdtype(dtype)))
+    for b in range(B):
+        m = lens[b]
+        k, v, x = K[b, :, :m].double(), V[b, :, :m].double(), q[b].double().view(Hkv, -1, T, d)
+        S = (x.reshape(Hkv, -1, d) @ k.transpose(1, 2) * c.scale).view(Hkv, -1, T, m)
+        S = S.masked_fill(torch.arange(m, device=U.DEV) > m - T + torch.arange(T, device=U.DEV)[:, None], -torch.inf)
+        top = S.amax(-1, keepdim=True).clamp(min=-1e300)
+        w = (S - top).exp()
+        l = w.sum(-1, keepdim=True)
+        Yr = ((w.view(Hkv, -1, m) @ v).view(Hkv, -1, T, d) / l.clamp(min=1e-300)).view(Hq, T, d).cpu().numpy()
+        Lr = (top + l.log()).view(Hq, T).cpu().numpy()
+        A = c.scale * (x.abs().reshape(Hkv, -1, d) @ k.abs().transpose(1, 2)).amax(-1).view(Hq, T).cpu().numpy()
+        delta = (d + 8) * 2.0 ** -24 * A + 2.0 ** -22 * (1 + A)
+        p, half = (2.0 ** -17, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -24, 2.0 ** -24)
+        tol = half * np.abs(Yr) + ((2 * delta + p + 2 * m * 2.0 ** -24) * float(v.abs().max()))[..., None]
+        assert np.isfinite(Y[b]).all() and (np.abs(Y[b] - Yr) <= tol).all(), (np.abs(Y[b] - Yr) - tol).max()
+        assert np.array_equal(np.isneginf(L[b]), np.isneginf(Lr))
+        seen = np.isfinite(Lr)
+        assert (np.abs(L[b][seen] - Lr[seen]) <= (delta + m * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(Lr)))[seen]).all()
+
+
+@pytest.mark.parametrize("what", [float("inf"), float("nan")])
+@pytest.mark.parametrize("T,n", [(1, 300), (5, 300), (300, 6500)])
+def test_queries_with_infinities_and_nan(what, T, n):
+    """Their own results are NaN, the others' are as if they were not there"""
+    c = Setup(1, 8, 2, 128, 64, -(-n // 64), "bf16", seed=T)
+    c.dev(c.table)
+    K, V = (torch.randn(1, 2, n, 128, device=U.DEV).to(torch.bfloat16) for _ in "KV")
+    sa().sa_cache4_write(c.desc, K, V, None, None, c.dev(c.table), c.pool)
+    q, Y, L = c.decode(T, [n])
+    q[0, 3, T // 2, 77] = what
+    _, Y2, L2 = c.decode(T, [n], q=q)
+    assert np.isnan(Y2[0, 3, T // 2]).all() and np.isnan(L2[0, 3, T // 2])
+    Y2[0, 3, T // 2], L2[0, 3, T // 2] = Y[0, 3, T // 2], L[0, 3, T // 2]
+    assert np.array_equal(Y, Y2) and np.array_equal(L, L2)
+
+
 def test_one_cached_row_comes_back_as_it_is():
     c = Setup(1, 4, 2, 128, 32, 1, "bf16", seed=8)
     c.write(c.rows(1), c.rows(1))
