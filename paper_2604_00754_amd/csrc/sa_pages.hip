@@ -17,7 +17,7 @@ __device__ __forceinline__ bool is_page(const Tables& t, int x) { return (unsign
 // pages of the first `rows` rows (clamped to 0..capacity)
 __device__ __forceinline__ int pages_of(const Tables& t, int rows) {
   const int r = min(max(rows, 0), t.capacity);
-  return (int)(((long)r + (1 << t.rows_log2) - 1) >> t.rows_log2);
+  return (r + (1 << t.rows_log2) - 1) >> t.rows_log2;  // (the capacity is at most 2^30)
 }
 
 __global__ __launch_bounds__(256) void copy_ints_kernel(const int32_t* from, int32_t* to, int n) {
@@ -95,17 +95,17 @@ __device__ __forceinline__ int scan_before(int v, int* area, int* total) {
   return before + s - v;
 }
 
-// Pages are looked through kLook at a time, kLookEach of them a lane: position at + 512 wave + 64 i + lane of the order.
-constexpr int kLookEach = 8, kLook = kDecide * kLookEach;
-__device__ __forceinline__ int look_place(int i) { return (threadIdx.x >> 6) * (64 * kLookEach) + 64 * i + (threadIdx.x & 63); }
+// Pages are looked through kLook at a time, kLookEach of them a lane: position at + 256 wave + 64 i + lane of the order.
+constexpr int kLookEach = 4, kLook = kDecide * kLookEach;
+__device__ __forceinline__ unsigned look_place(int i) { return (threadIdx.x >> 6) * (64 * kLookEach) + 64 * i + (threadIdx.x & 63); }
 // Bit i: the lane's page number i of those from position `at` on, upwards from lo or downwards from hi - 1, is free (FREE) or in use.
 template <bool UP, bool FREE>
-__device__ __forceinline__ int look(const int32_t* refs, int lo, int hi, long at) {
+__device__ __forceinline__ int look(const int32_t* refs, int lo, int hi, unsigned at) {
   int n[kLookEach], flags = 0;
 #pragma unroll
   for (int i = 0; i < kLookEach; ++i) {
-    const long k = at + look_place(i);
-    n[i] = k < hi - lo ? refs[UP ? lo + (int)k : hi - 1 - (int)k] : (FREE ? 1 : 0);
+    const unsigned k = at + look_place(i);
+    n[i] = k < (unsigned)(hi - lo) ? refs[UP ? lo + k : hi - 1 - k] : (FREE ? 1 : 0);
   }
 #pragma unroll
   for (int i = 0; i < kLookEach; ++i) flags |= (n[i] <= 0) == FREE ? 1 << i : 0;
@@ -118,7 +118,7 @@ template <bool UP, bool FREE>
 __device__ __forceinline__ int collect(const int32_t* refs, int lo, int hi, int want, int flags, int32_t* list, int* area) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int found = 0;
-  for (long at = 0; at < hi - lo && found < want; at += kLook) {
+  for (unsigned at = 0; at < (unsigned)(hi - lo) && found < want; at += kLook) {
     if (at > 0) flags = look<UP, FREE>(refs, lo, hi, at);
     int mine = 0;
 #pragma unroll
@@ -138,8 +138,8 @@ __device__ __forceinline__ int collect(const int32_t* refs, int lo, int hi, int 
       const unsigned long long who = __ballot(flags >> i & 1);
       if (flags >> i & 1) {
         const int at_list = k + __popcll(who & ((1ull << lane) - 1));
-        const long j = at + look_place(i);
-        if (at_list < want) list[at_list] = UP ? lo + (int)j : hi - 1 - (int)j;
+        const unsigned j = at + look_place(i);
+        if (at_list < want) list[at_list] = UP ? lo + j : hi - 1 - j;
       }
       k += __popcll(who);
     }
@@ -164,7 +164,7 @@ struct ExtendArgs {
 struct Touched { int first, last, begun; };  // entries first..last-1; the first holds rows already
 __device__ __forceinline__ Touched touched(const Tables& t, int len, int add) {
   const int a = min(max(len, 0), t.capacity);
-  const int b = (int)min((long)a + max(add, 0), (long)t.capacity);
+  const int b = a + min(max(add, 0), t.capacity - a);
   Touched x;
   x.first = a >> t.rows_log2;
   x.last = b > a ? pages_of(t, b) : x.first;
