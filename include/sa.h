@@ -301,7 +301,7 @@ sa_status sa_bwd(const sa_desc* sa, const sa_desc* swa,
  * (rows and columns lie as the lanes of the matrix instructions take them.)  A position p of sequence b is row
  * p % page_rows of page table[b][p / page_rows]; table is int32 [B, max_pages], shared by the layers.  An entry outside
  * 0..pages-1 is a page that is not there: rows written to it are dropped, its rows read back as zeros and are not seen by attention.
- * Nothing outside the pool is touched whatever the tables hold. */
+ * Nothing outside the pool is touched whatever the tables hold.  A workspace serves one call at a time. */
 typedef struct {
   int32_t B, Hq, Hkv, d;  /* sequences, heads (Hq % Hkv == 0), d in {64,128}                        */
   int32_t page_rows;      /* rows of a page: a power of two, 32 .. 1024                             */
@@ -310,7 +310,8 @@ typedef struct {
   int32_t layers;         /* layers of the pool, for the calls that move pages (sa_pages_*)         */
   int32_t dtype;          /* sa_dtype of q, Y and of the K and V rows written and read              */
   float scale;            /* softmax scale; <= 0 selects 1/sqrt(d) (Eq. 1)                          */
-} sa_cache4_desc;         /* SA_ERR_SHAPE beyond: B*max_pages < 2^31, pages*Hkv*page_rows/32 < 2^31 */
+} sa_cache4_desc;         /* SA_ERR_SHAPE beyond: B, layers <= 65535, pages of at most 2^30 bytes (all heads of a layer),
+                             B*max_pages, pages*layers, pages*Hkv*page_rows/32 < 2^31               */
 
 /* Bytes of the pool, of all layers (0 for an invalid descriptor). */
 size_t sa_cache4_pool_bytes(const sa_cache4_desc* desc);
@@ -337,7 +338,7 @@ sa_status sa_cache4_read(const sa_cache4_desc* desc, const void* pool, const int
  * device): rows of each sequence, the T tokens' own included, clamped to 0..max_len on the device; max_len (host,
  * 1 <= max_len <= max_pages*page_rows) sizes the launch.  Token t sees the positions <= lens[b] - T + t whose pages are there;
  * one that sees none gets Y = 0 and LSE = -inf.  B*Hq*T < 2^31 (SA_ERR_SHAPE).
- * Scores, softmax and sums are fp32; K and V enter exactly, probabilities with 17 bits (bf16) or 24 (fp32).
+ * Scores, softmax and sums are fp32; q, K and V enter exactly, probabilities with 11 bits (bf16) or 22 (fp32) or more.
  * ws: sa_cache4_workspace_bytes(desc, SA_OP_CACHE4_DECODE, T) bytes (may be NULL if that is 0). */
 sa_status sa_cache4_decode_fwd(const sa_cache4_desc* desc, const void* q, int32_t T, const void* pool,
                                const int32_t* table, const int32_t* lens, int32_t max_len, void* Y, float* LSE,

@@ -138,20 +138,22 @@ size_t gated_fwd_workspace(const sa_desc* c) {
   return align256((size_t)c->B * c->Hq * c->n * c->d * 2);
 }
 
-// A cache in 4 bits.  Sizes are kept where 32-bit numbers of tiles, table entries, positions and query rows hold.
+// A cache in 4 bits.  Sizes are kept where 32-bit numbers of tiles, table entries, positions and bytes of a page hold, and launches
+// of a workgroup for each sequence and layer.
 sa_status validate_cache4(const sa_cache4_desc* c) {
   if (!c) return SA_ERR_NULL;
   if (c->B < 1 || c->Hq < 1 || c->Hkv < 1 || c->pages < 1 || c->max_pages < 1 || c->layers < 1) return SA_ERR_SHAPE;
+  if (c->B > 65535 || c->layers > 65535) return SA_ERR_SHAPE;
   if (c->Hq % c->Hkv != 0) return SA_ERR_SHAPE;
   if (!(c->scale == c->scale) || isinf(c->scale)) return SA_ERR_SHAPE;
   if (!(c->d == 64 || c->d == 128)) return SA_ERR_UNSUPPORTED;
   if (!(c->dtype == SA_BF16 || c->dtype == SA_F32)) return SA_ERR_UNSUPPORTED;
   if (c->page_rows < 32 || c->page_rows > 1024 || (c->page_rows & (c->page_rows - 1)) != 0) return SA_ERR_UNSUPPORTED;
-  const long long tiles = c->page_rows / 32;
-  if ((long long)c->max_pages * c->page_rows > (1ll << 30) || (long long)c->B * c->max_pages > 0x7fffffffll) return SA_ERR_SHAPE;
-  if ((long long)c->pages * c->Hkv > 0x7fffffffll / tiles) return SA_ERR_SHAPE;
-  if ((long long)c->B * c->Hq > 0x7fffffffll) return SA_ERR_SHAPE;
-  if (c->Hkv > 0x7fffffffll / (tiles * 34 * c->d)) return SA_ERR_SHAPE;  // bytes of a page
+  const long long tiles = c->page_rows / 32, most = 0x7fffffffll;
+  if ((long long)c->max_pages * c->page_rows > (1ll << 30) || (long long)c->B * c->max_pages > most) return SA_ERR_SHAPE;
+  if ((long long)c->pages * c->Hkv > most / tiles || (long long)c->pages * c->layers > most) return SA_ERR_SHAPE;
+  if ((long long)c->B * c->Hq > most) return SA_ERR_SHAPE;
+  if (c->Hkv > (1ll << 30) / (tiles * 34 * c->d)) return SA_ERR_SHAPE;
   return SA_OK;
 }
 
@@ -743,7 +745,6 @@ sa_status sa_pages_extend(const sa_cache4_desc* c, const int32_t* lens, const in
   if (s != SA_OK) return s;
   if (!lens || !add || !table || !refs || !pool || !info) return SA_ERR_NULL;
   if (!aligned_to(16, {pool, ws}) || !aligned_to(4, {lens, add, table, refs, info})) return SA_ERR_UNSUPPORTED;
-  if (c->B > 65535 || c->layers > 65535) return SA_ERR_UNSUPPORTED;
   if (!ws || ws_bytes < sa::pages_extend_workspace_bytes(c)) return SA_ERR_WORKSPACE;
   return hip_status(sa::launch_pages_extend(c, lens, add, table, refs, pool, info, ws, (hipStream_t)stream));
 }

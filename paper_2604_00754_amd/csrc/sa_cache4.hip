@@ -331,9 +331,15 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a)
 //   with query row c and cached rows 4 g + i of each half;
 //   O^T (16 elements x 16 query rows, D/16 times) += V^T P^T, where those scores are the operand P^T as they stand and lane (r, g) holds
 //   elements E r .. E r + E - 1 of the same 8 cached rows: the order in which V lies in the tile.
-// 4-bit codes become bf16 pairs by one conversion each, which multiplies by the power of two as well; V's pairs are re-paired
-// over two rows by byte permutes.  The maximum of a query row is raised only where a score passes it by more than 2^8: the
-// sums stay far inside fp32's range, and the usual tile needs no exchange between lanes and no product with a correction.
+// No operand passes through LDS.  4-bit codes become pairs by one conversion each, which multiplies by the power of two as well; V's
+// pairs are re-paired over two rows by byte permutes.  K and q are bf16 (fp32 q: three parts of 8 bits), V and the probabilities
+// f16, whose 11 bits keep a probability eight times as well as bf16's would (fp32: two parts); where a tile's scales of V are out of
+// f16's reach the wave's tiles are gone through again in bf16 with a part more.
+// Bound.  One token: the K/V rows once, d + d/16 bytes a row, HBM: 16 x 8192 rows of 8 KV heads of 128 (143 MB) 31 us with the
+// merge, the kernel itself 5.3 TB/s; a tile is 184 vector instructions, which bound the chip at 11 TB/s.  Many tokens: the vector ALU
+// (T509 over 32768 rows, 32 / 8 heads 296 us, 0.92 PFLOP/s: 84 % of its cycles, the matrix pipe 40 %): of 254 instructions for 32 query rows
+// half unpack the tile.  Sharing that over the waves of a workgroup through LDS left 150 and took as long, LDS reads and barriers in
+// its place; 48 rows a wave 302 us, 64 rows 433 (one wave a SIMD).
 struct AttnArgs {
   Cache c;
   const void* q;
@@ -345,8 +351,8 @@ struct AttnArgs {
   float scale_log2e;
 };
 
-// The maximum is raised where a score passes it by more than this; the largest probability is then 2^15, with the lift, and the smallest
-// that f16 holds to all its bits 2^-21 of the largest possible.
+// The maximum is raised where a score passes it by more than 2^kRaise: the usual tile needs no exchange between lanes and no product with a
+// correction.  With the lift the largest probability is 2^15, a row's own largest at least 2^7, and f16 holds all its bits down to 2^-14.
 // kNone: the maximum before a row has been seen, a finite number (a row that is not seen has the score -inf).
 constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.0e38f;
 
@@ -379,7 +385,6 @@ __device__ __forceinline__ void split_pair_f16(float x, float y, uint32_t* w) {
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma16(f16x8 a, f16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
-
 
 // A lane's part of a tile: loads through a buffer descriptor of the tile, whose base is scalar and whose offsets are four numbers a lane keeps.
 typedef __amdgpu_buffer_rsrc_t tile_buffer;
@@ -425,7 +430,7 @@ struct TileRegs {
 // the two elements of a byte of the word, as pairs of V (bf16x8: bf16, f16x8: f16)
 template <typename V, int SEL>
 __device__ __forceinline__ uint32_t two_values(uint32_t codes, float scale) {
-  if constexpr (sizeof(V) == sizeof(bf16x8) && __is_same(V, bf16x8)) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
+  if constexpr (__is_same(V, bf16x8)) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, SEL));
   else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, scale, SEL));
 }
 template <typename V>
@@ -817,6 +822,9 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(con
   }
 }
 
+// a launch of n workgroups: the threads of one dimension are counted in 32 bits
+bool fits_a_launch(long n, int threads) { return n <= 0xffffffffL / threads; }
+
 int log2_of(int v) { int k = 0; while ((1 << k) < v) ++k; return k; }
 
 Cache cache_of(const sa_cache4_desc* c, void* pool, const int32_t* table) {
@@ -875,16 +883,16 @@ Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
 template <typename T, int D>
 hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, const Plan& p, hipStream_t st) {
   const long blocks = (long)c->B * c->Hkv * a.row_blocks * a.splits;
-  if (blocks > 0x7fffffffL) return hipErrorNotSupported;
+  const long rows = (long)c->B * c->Hq * a.T;
+  if (!fits_a_launch(blocks, 512) || (a.splits > 1 && !fits_a_launch(rows, a.splits <= 16 ? 64 : 512))) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
   if (p.nt == 1) cache4_attn_kernel<T, D, 1, waves_of(1)><<<grid, 64 * waves_of(1), 0, st>>>(a);
   else cache4_attn_kernel<T, D, 2, waves_of(2)><<<grid, 64 * waves_of(2), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  const int rows = c->B * c->Hq * a.T;
   T* Y = reinterpret_cast<T*>(a.Y);
-  if (a.splits <= 16) cache4_merge_kernel<T, D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, Y, a.LSE, a.splits, rows);
-  else cache4_merge_kernel<T, D, 8><<<(unsigned)rows, 512, 0, st>>>(a.part, Y, a.LSE, a.splits, rows);
+  if (a.splits <= 16) cache4_merge_kernel<T, D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, Y, a.LSE, a.splits, (int)rows);
+  else cache4_merge_kernel<T, D, 8><<<(unsigned)rows, 512, 0, st>>>(a.part, Y, a.LSE, a.splits, (int)rows);
   return hipGetLastError();
 }
 
@@ -897,7 +905,7 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
   a.starts = starts; a.counts = counts; a.K = K; a.V = V; a.T = T;
   a.tiles = (int)(((long)T + 62) / kTile);  // the first and the last may be begun
   const long blocks = (long)c->B * c->Hkv * ((2 * (long)a.tiles + kRowWaves - 1) / kRowWaves);
-  if (blocks > 0x7fffffffL) return hipErrorNotSupported;
+  if (!fits_a_launch(blocks, kRowWaves * 64)) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
   const dim3 block(kRowWaves * 64);
   const bool bf16 = c->dtype == SA_BF16;

@@ -90,9 +90,10 @@ def test_null_descriptor():
     ("page_rows", 16, sa.SA_ERR_UNSUPPORTED), ("page_rows", 96, sa.SA_ERR_UNSUPPORTED), ("page_rows", 2048, sa.SA_ERR_UNSUPPORTED),
     ("page_rows", 0, sa.SA_ERR_UNSUPPORTED), ("page_rows", -64, sa.SA_ERR_UNSUPPORTED),
     ("max_pages", (1 << 30) // 64 + 1, sa.SA_ERR_SHAPE), ("B", 1 << 27, sa.SA_ERR_SHAPE), ("pages", 1 << 29, sa.SA_ERR_SHAPE),
+    ("B", 65536, sa.SA_ERR_SHAPE), ("layers", 65536, sa.SA_ERR_SHAPE), ("Hkv", 2 * 123362, sa.SA_ERR_SHAPE),
 ])
 def test_bad_descriptors(field, value, status):
-    d = desc(**{field: value})
+    d = desc(**{field: value}, **({"Hq": value} if field == "Hkv" and value > 3 else {}))
     assert set(calls(d).values()) == {status}
     assert sa.sa_cache4_pool_bytes(d) == 0 and sa.sa_cache4_workspace_bytes(d, sa.SA_OP_CACHE4_DECODE, 1) == 0
 
@@ -178,6 +179,21 @@ def test_outputs_that_overlap_inputs():
     name = "sa_pages_compact"
     assert calls(d, table_out=C.c_void_p(4096 + 4))[name] == sa.SA_ERR_UNSUPPORTED
     assert calls(d, refs_out=C.c_void_p(4096 + 39 * 4))[name] == sa.SA_ERR_UNSUPPORTED
+
+
+def test_sizes_at_their_limits():
+    """Accepted: the next argument error is what is reported (sizes are judged before the tensors)"""
+    for d in (desc(B=65535, max_pages=16), desc(layers=65535), desc(pages=(1 << 31) // 4 - 1, layers=1), desc(max_pages=(1 << 30) // 64, B=1),
+              desc(Hkv=123361, Hq=123361, page_rows=64, B=1, pages=2, layers=1)):
+        assert set(calls(d, table=None).values()) == {sa.SA_ERR_NULL} and sa.sa_cache4_pool_bytes(d) > 0
+    for d in (desc(pages=40000, layers=60000), desc(pages=1 << 30, Hkv=1, layers=1)):
+        assert set(calls(d, table=None).values()) == {sa.SA_ERR_SHAPE}
+
+
+def test_calls_that_need_more_workgroups_than_a_launch_holds():
+    d = desc(B=1, Hq=1, Hkv=1, max_pages=1 << 24, layers=1)
+    got = calls(d, T=(1 << 31) - 1)
+    assert got["sa_cache4_write"] == got["sa_cache4_read"] == sa.SA_ERR_UNSUPPORTED
 
 
 def test_pool_size():

@@ -218,6 +218,48 @@ def decode(desc, q, pool, table, lens, max_len):
     return Y
 
 
+def test_pools_beyond_4_gib():
+    """Pages whose bytes lie past 2^32 of a layer: written, read, attended to, copied and moved as in a small pool"""
+    Hkv, d, R, M, P = 8, 128, 64, 4, 66000
+    big, small = (sa().make_cache4_desc(2, 16, Hkv, d, R, p, M, 1) for p in (P, 8))
+    assert sa().sa_cache4_pool_bytes(big) > 1.05 * 2 ** 32
+    pool = torch.zeros(sa().sa_cache4_pool_bytes(big), dtype=torch.uint8, device=U.DEV)
+    near = torch.zeros(sa().sa_cache4_pool_bytes(small), dtype=torch.uint8, device=U.DEV)
+    far_table, near_table = dev([[P - 1, 5, P - 2, 61700], [P - 3, P - 1, -1, -1]]), dev([[0, 1, 2, 3], [4, 0, -1, -1]])
+    g = torch.Generator(device=U.DEV).manual_seed(3)
+    K, V = (torch.randn(2, Hkv, 256, d, device=U.DEV, generator=g).to(torch.bfloat16) for _ in "KV")
+    q = torch.randn(2, 16, 3, d, device=U.DEV, generator=g).to(torch.bfloat16)
+    counts, lens = dev([256, 64]), dev([250, 100])
+
+    def read(desc, pool, table):
+        k, v = torch.zeros_like(K), torch.zeros_like(K)
+        sa().sa_cache4_read(desc, pool, table, None, lens, k, v)
+        return k, v, decode(desc, q, pool, table, lens, 256)
+
+    for desc, p, table in ((big, pool, far_table), (small, near, near_table)):
+        sa().sa_cache4_write(desc, K, V, None, counts, table, p)
+    want = read(small, near, near_table)
+    for a, b in zip(read(big, pool, far_table), want):
+        assert torch.equal(a, b)
+    # a page of its own for the second sequence's rows past 100, copied from the last page of the pool into the last but ten
+    refs = torch.ones(P, dtype=torch.int32, device=U.DEV)
+    refs[P - 1], refs[P - 11] = 2, 0
+    info = torch.zeros(2, dtype=torch.int32, device=U.DEV)
+    ws = torch.empty(max(sa().sa_cache4_workspace_bytes(big, op) for op in (sa().SA_OP_PAGES_EXTEND, sa().SA_OP_PAGES_COMPACT)), dtype=torch.uint8, device=U.DEV)
+    sa().sa_pages_extend(big, lens, dev([0, 9]), far_table, refs, pool, info, ws)
+    assert info.tolist() == [1, 0] and far_table.tolist() == [[P - 1, 5, P - 2, 61700], [P - 3, P - 11, -1, -1]]
+    for a, b in zip(read(big, pool, far_table), want):
+        assert torch.equal(a, b)
+    # only the pages in the table stay: they move to the front
+    refs.zero_()
+    refs[far_table[far_table >= 0].long()] = 1
+    sa().sa_pages_compact(big, P, far_table, refs, far_table, refs, pool, info, ws)
+    assert info.tolist() == [6, 5] and int(far_table.max()) == 5 and refs.tolist()[:7] == [1] * 6 + [0]
+    pool[6 * (pool.numel() // P):] = 255
+    for a, b in zip(read(big, pool, far_table), want):
+        assert torch.equal(a, b)
+
+
 def test_a_serving_loop():
     """Prompts, beams that share them, drafted tokens that are taken back, a sequence that ends, compaction in between: after every
     step each sequence's attention is, bit for bit, what a cache of its own with the same rows gives."""
