@@ -289,8 +289,8 @@ sa_status sa_bwd(const sa_desc* sa, const sa_desc* swa,
  * Format (the FP4 of the OCP Microscaling formats): an element is E2M1, sign and magnitude 0 .5 1 1.5 2 3 4 6 (codes
  * 0..7); 32 neighbouring elements of a row share a power of two 2^e, held as the byte e + 127.  With amax the largest
  * magnitude of the 32, e = floor(log2 amax) - 2, and one more if amax / 2^e > 7 (8 is then as near as 6 or nearer); at
- * least -125, so that every value held is a normal bf16 number and is exact in both dtypes; 0 for 32 zeros.  Elements are rounded to the nearest, ties to the even
- * code, those above 6 to 6.  A row whose K or V has an infinity or NaN in a KV head is held as such in that head (scale
+ * least -125 and at most 125, so that every value held is a normal bf16 number and is exact in both dtypes; 0 for 32 zeros.
+ * Elements are rounded to the nearest, ties to the even code, those above 6 to 6.  A row whose K or V has an infinity or NaN in a KV head is held as such in that head (scale
  * bytes of K 255, of V 127, codes 0): it reads back as NaN in K and V and makes Y and LSE of every query that sees it NaN; queries that do
  * not see it are as if it were not there.
  *

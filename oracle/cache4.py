@@ -16,7 +16,7 @@ def block_exponent(amax: float) -> int:
     e = math.frexp(amax)[1] - 1 - 2   # floor(log2 amax) - 2
     if amax / 2.0 ** e > 7:
         e += 1
-    return max(e, -125)
+    return min(max(e, -125), 125)
 
 
 def element_code(x: float, e: int) -> int:

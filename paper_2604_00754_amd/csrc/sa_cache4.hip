@@ -127,11 +127,12 @@ struct Elements<float, E> {
   }
 };
 
-// The scale byte of a block whose largest magnitude has the bits `top`: its exponent less 2, one more past 1.75 (7/4) of the power.
+// The scale byte of a block whose largest magnitude has the bits `top`: its exponent less 2, one more past 1.75 (7/4) of the power;
+// held to 2 (every value a normal number) .. 252 (4 * 2^126 would be none).
 constexpr uint32_t kNoRow = 255, kOne = 127;
 __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   const int e = (int)(top >> 23) - 2 + ((top & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return top == 0 ? kOne : (uint32_t)(e < 2 ? 2 : e);
+  return top == 0 ? kOne : (uint32_t)min(max(e, 2), 252);
 }
 
 struct RowsArgs {

@@ -43,6 +43,12 @@ def test_normal_rows_are_held_as_well_as_the_better_of_two_powers_holds_them():
     assert err <= 1.02 * best and np.sqrt(err / (x ** 2).sum()) < 0.115
 
 
+def test_the_largest_numbers_are_held_as_numbers():
+    for amax in (7 * 2.0 ** 125, np.nextafter(7 * 2.0 ** 125, np.inf), float(np.finfo(np.float32).max)):
+        e = orc.block_exponent(amax)
+        assert e == 125 and orc.value(orc.element_code(amax, e), e + 127) == 6 * 2.0 ** 125
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_every_byte_of_a_tile_has_one_place(d):
     c = orc.Cache(1, d, 32, 1)

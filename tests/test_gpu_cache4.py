@@ -140,6 +140,24 @@ def test_values_at_the_edges_of_the_format(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_rows_come_back_finite(dtype, d):
+    """Above 7 * 2^125 the next power of two would hold 4 * 2^126, which is no number: 6 * 2^125 is held.  Queries of zeros see them evenly."""
+    c = Setup(1, 2, 1, d, 32, 2, dtype, seed=1)
+    top = torch.finfo(U.tdtype(dtype)).max
+    t = torch.full((1, 1, 40, d), top, device=U.DEV, dtype=U.tdtype(dtype))
+    t[:, :, 1::2] *= -1
+    zero = torch.zeros_like(t)
+    c.write((t, U.to_np64(t)), (zero, U.to_np64(zero)))
+    c.assert_bytes()
+    K, V = c.read(40, [0], None)
+    assert np.array_equal(K, np.sign(U.to_np64(t)) * 6 * 2.0 ** 125) and not V.any()
+    q = torch.zeros((1, 2, 1, d), device=U.DEV, dtype=U.tdtype(dtype))
+    _, Y, L = c.decode(1, [40], q=q)
+    assert not Y.any() and np.allclose(L, np.log(40), rtol=2.0 ** -20, atol=0)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_every_bf16_value_is_rounded_as_defined(dtype):
     """All magnitudes of one binade beside a largest of each of 8 kinds"""
     c = Setup(1, 1, 1, 128, 128, 1, dtype, seed=1)
