@@ -338,7 +338,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a)
 // f16's reach the wave's tiles are gone through again in bf16 with a part more.
 // Bound.  One token: the K/V rows once, d + d/16 bytes a row, HBM: 16 x 8192 rows of 8 KV heads of 128 (143 MB) 31 us with the
 // merge, the kernel itself 5.3 TB/s; a tile is 184 vector instructions, which bound the chip at 11 TB/s.  Many tokens: the vector ALU
-// (T509 over 32768 rows, 32 / 8 heads 296 us, 0.92 PFLOP/s: 84 % of its cycles, the matrix pipe 40 %): of 254 instructions for 32 query rows
+// (T509 over 32768 rows, 32 / 8 heads 296 us, 0.92 PFLOP/s: active in 88 % of the waves' cycles, the matrix pipe in 44 %): of 254 instructions for 32 query rows
 // half unpack the tile.  Sharing that over the waves of a workgroup through LDS left 150 and took as long, LDS reads and barriers in
 // its place; 48 rows a wave 302 us, 64 rows 433 (one wave a SIMD).
 struct AttnArgs {
