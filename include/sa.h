@@ -339,6 +339,8 @@ sa_status sa_cache4_read(const sa_cache4_desc* desc, const void* pool, const int
  * 1 <= max_len <= max_pages*page_rows) sizes the launch.  Token t sees the positions <= lens[b] - T + t whose pages are there;
  * one that sees none gets Y = 0 and LSE = -inf.  B*Hq*T < 2^31 (SA_ERR_SHAPE).
  * Scores, softmax and sums are fp32; q, K and V enter exactly, probabilities with 11 bits (bf16) or 22 (fp32) or more.
+ * Where the sums are cut depends on the sizes and, in a batch, on all of its lengths: a sequence's results agree between batches to
+ * the rounding above, between equal calls to the bit.
  * ws: sa_cache4_workspace_bytes(desc, SA_OP_CACHE4_DECODE, T) bytes (may be NULL if that is 0). */
 sa_status sa_cache4_decode_fwd(const sa_cache4_desc* desc, const void* q, int32_t T, const void* pool,
                                const int32_t* table, const int32_t* lens, int32_t max_len, void* Y, float* LSE,

@@ -118,6 +118,8 @@ def _load():
     lib.sa_internal_gate_kernel.argtypes = [dp, C.c_int, C.c_int]
     lib.sa_internal_cache4_plan.restype = C.c_int
     lib.sa_internal_cache4_plan.argtypes = [cp, C.c_int, C.c_int]
+    lib.sa_internal_cache4_dealt.restype = C.c_int
+    lib.sa_internal_cache4_dealt.argtypes = [cp, C.c_int, C.c_int]
     lib.sa_internal_gate_dw_pieces.restype = C.c_int
     lib.sa_internal_gate_dw_pieces.argtypes = [dp, C.c_int]
     lib.swa_fwd.restype = C.c_int
@@ -355,6 +357,12 @@ def cache4_plan(desc, T, max_len):
     """How sa_cache4_decode_fwd deals a call: (blocks of 16 query rows a wave takes, pieces of the cache)."""
     p = _lib.sa_internal_cache4_plan(C.byref(desc), int(T), int(max_len))
     return p & 3, p >> 2
+
+
+def cache4_dealt(desc, T, max_len):
+    """Workgroups of a sequence (for each KV head and block of query rows) where sa_cache4_decode_fwd deals all of them by the sequences'
+    lengths if those differ much, else 0."""
+    return _lib.sa_internal_cache4_dealt(C.byref(desc), int(T), int(max_len))
 
 
 def raw():

@@ -720,6 +720,11 @@ int sa_internal_cache4_plan(const sa_cache4_desc* c, int T, int max_len) {
   return sa::cache4_decode_plan(c, T, max_len);
 }
 
+int sa_internal_cache4_dealt(const sa_cache4_desc* c, int T, int max_len) {
+  if (validate_cache4(c) != SA_OK || !cache4_rows_ok(c, T) || max_len < 1 || max_len > c->max_pages * c->page_rows) return 0;
+  return sa::cache4_decode_dealt(c, T, max_len);
+}
+
 sa_status sa_pages_fork(const sa_cache4_desc* c, const int32_t* parents, const int32_t* table, const int32_t* lens,
                         const int32_t* refs, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, void* stream) {
   sa_status s = validate_cache4(c);

@@ -346,10 +346,20 @@ struct AttnArgs {
   const void* q;
   void* Y;
   float* LSE;
-  float* part;  // [B*Hq*T][splits][D + 2]: weighted V sum, maximum (log2 domain), sum
+  float* part;  // [Hkv][rows][B*splits][D + 2]: weighted V sum, maximum (log2 domain), sum
+  int32_t* dealt;  // [2][64]: a sequence's first piece and their number, or NULL: splits of them each
   const int32_t* lens;
-  int T, rows, row_blocks, max_len, chunk, splits;
+  int T, rows, row_blocks, max_len, chunk, splits, pieces;
+  uint32_t few;  // tiles of all sequences below which pieces are dealt by length
   float scale_log2e;
+};
+
+struct MergeArgs {
+  const float* part;
+  const int32_t* dealt;
+  void* Y;
+  float* LSE;
+  int rows, splits, pieces, all;  // rows of a sequence, all KV heads; all: slots of all sequences
 };
 
 // The maximum is raised where a score passes it by more than 2^kRaise: the usual tile needs no exchange between lanes and no product with a
@@ -560,6 +570,41 @@ __device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, flo
   }
 }
 
+// Sum of v over this lane and those before it.
+__device__ __forceinline__ int sum_up_to(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);  // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, true);  // row_bcast 15 into rows 1 and 3
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, true);  // row_bcast 31 into rows 2 and 3
+  return v;
+}
+
+// How many of the `slots` = B splits pieces lane b's sequence of t tiles gets, so that no piece is much longer than the others: one more than
+// t r, rounded down, where r is as large as the slots allow (up to 1/32 of what lies between a rate that always fits and one that cannot),
+// none of less than W tiles, and as many as a wave's lists need.
+template <int W, int LISTS>
+__device__ __forceinline__ int pieces_of(int t, uint32_t tiles, int B, int splits) {
+  constexpr int kWhole = 64 * LISTS * W;
+  const int slots = B * splits;
+  const int least = (t + kWhole - 1) / kWhole, all = (t + W - 1) / W;
+  const auto dealt = [&](float r) { return min(max((int)((float)t * r) + 1, least), all); };
+  const float total = fmaxf(1.f, (float)tiles);
+  float lo = (float)(slots - B) / total, hi = (float)slots / total;
+  int best = min(splits, all);
+#pragma unroll 1
+  for (int i = 0; i < 6; ++i) {
+    const float r = i == 0 ? lo : 0.5f * (lo + hi);
+    const int n = dealt(r);
+    const bool fits = __builtin_amdgcn_readlane(sum_up_to(n), 63) <= slots;
+    best = fits ? n : best;
+    lo = fits ? r : lo;
+    hi = fits || i == 0 ? hi : r;
+  }
+  return best;
+}
+
 // Lists of 64 tiles that a wave keeps the numbers of.
 constexpr int lists_of(int nt) { return nt == 1 ? 1 : 2; }
 // Wavefronts a SIMD that the registers are kept for: what the compiler reaches without spilling.
@@ -578,28 +623,60 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
   __shared__ float lds_ml[W][16][2];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
-  const int split = (int)(blockIdx.x % (unsigned)a.splits);
+  int split = (int)(blockIdx.x % (unsigned)a.splits);
   const unsigned rest = blockIdx.x / (unsigned)a.splits;
   const int rb = (int)(rest % (unsigned)a.row_blocks);
-  const int bh = (int)(rest / (unsigned)a.row_blocks);
-  const int hk = bh % a.c.Hkv, b = bh / a.c.Hkv;
-  const int row0 = rb * 16 * NT;
+  int b = (int)(rest / (unsigned)a.row_blocks / (unsigned)a.c.Hkv);
+  const int hk = (int)(rest / (unsigned)a.row_blocks) - b * a.c.Hkv;
+  const int row0 = rb * 16 * NT, slot = b * a.splits + split;
   // The numbers of the wave's tiles (64 kLists at most), one a lane: of every tile that the longest sequence could have, so that the page
   // table's entries arrive together with the sequence's length and not behind it.
-  const int first = split * a.chunk + wave, end = min((split + 1) * a.chunk, (a.max_len + kTile - 1) / kTile);
-  int numbers[kLists];
+  const int bound = (a.max_len + kTile - 1) / kTile;
+  int first, end, pieces = a.pieces, numbers[kLists];
+  const auto take = [&](int chunk) {
+    first = split * chunk + wave;
+    end = min((split + 1) * chunk, bound);
 #pragma unroll
-  for (int k = 0; k < kLists; ++k) {
-    const int tile = first + W * (64 * k + lane);
-    numbers[k] = tile < end ? tile_number(a.c, b, hk, tile) : -1;
+    for (int k = 0; k < kLists; ++k) {
+      const int tile = first + W * (64 * k + lane);
+      numbers[k] = tile < end ? tile_number(a.c, b, hk, tile) : -1;
+    }
+  };
+  // (dealt: lane b holds the length of sequence b; the last slots may hold no piece)
+  const int held = a.dealt ? a.lens[min(lane, a.c.B - 1)] : a.lens[b];
+  take(a.chunk);
+  int len = min(max(held, 0), a.max_len);
+  if (a.dealt) {
+    const int rows = lane < a.c.B ? len : 0, t = (rows + kTile - 1) / kTile;
+    const uint32_t total = __builtin_amdgcn_readlane(sum_up_to(t), 63);
+    int from = lane * a.splits, n = a.pieces;
+    if (__builtin_expect(total < a.few, 0)) {
+      n = pieces_of<W, kLists>(t, total, a.c.B, a.splits);
+      const int upto = sum_up_to(n);
+      from = upto - n;
+      const unsigned long long behind = __ballot(upto > slot);
+      b = behind ? __builtin_ctzll(behind) : 0;
+      split = slot - __builtin_amdgcn_readlane(from, b);
+      pieces = __builtin_amdgcn_readlane(n, b);
+      const int tiles = __builtin_amdgcn_readlane(t, b);
+      if (behind) take((tiles + pieces - 1) / pieces);
+      else pieces = 0;
+    }
+    if (__builtin_expect(blockIdx.x == 0 && wave == 0, 0)) {
+      a.dealt[lane] = from;
+      a.dealt[64 + lane] = n;
+    }
+    if (split >= pieces) return;
+    len = __builtin_amdgcn_readlane(rows, b);
   }
+  len = __builtin_amdgcn_readfirstlane(len);
+  const int bh = b * a.c.Hkv + hk;
   const auto number_of = [&](int i) {
     int n = __builtin_amdgcn_readlane(numbers[0], i & 63);
 #pragma unroll
     for (int k = 1; k < kLists; ++k) n = i >> 6 == k ? __builtin_amdgcn_readlane(numbers[k], i & 63) : n;
     return n;
   };
-  const int len = __builtin_amdgcn_readfirstlane(min(max(a.lens[b], 0), a.max_len));
 
   // the last position each of the lane's query rows sees (-1 or less: none), and their largest and smallest over the block
   int last[NT];
@@ -733,11 +810,11 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
         sum = fmaf(f, lds_ml[w][c][1], sum);
       }
       const size_t out = (size_t)bh * a.rows + row;
-      if (a.splits == 1) {
+      if (pieces == 1) {
         store_y(reinterpret_cast<T*>(a.Y) + out * D + e, sum == 0.f ? 0.f : v / sum);
         if (e == 0 && a.LSE) a.LSE[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
       } else {
-        float* to = a.part + (out * a.splits + split) * (D + 2);
+        float* to = a.part + (((size_t)hk * a.rows + row) * (a.c.B * a.splits) + slot) * (D + 2);
         to[e] = v;
         if (e == 0) {
           to[D] = M;
@@ -751,26 +828,43 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
 // Joins the splits' results of a query row, W waves a row (one of them: four rows a workgroup, nothing exchanged): a wave
 // runs over its own splits with a running maximum, several of them in flight.
 template <typename T, int D, int W>
-__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(const float* __restrict__ part, T* __restrict__ Y,
-                                                                             float* __restrict__ LSE, int splits, int rows) {
+__global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(MergeArgs a) {
   constexpr int EPL = D / 64, UM = 8;
   __shared__ float lds_m[W], lds_l[W], lds_o[W][D];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int row = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
-  if (row >= rows) return;  // (W = 1)
-  const float* P = part + (size_t)row * splits * (D + 2);
-  float m = -INFINITY, l = 0.f, o[EPL] = {};
-  for (int s0 = W == 1 ? 0 : wave; s0 < splits; s0 += W * UM) {
-    float mx[UM], lx[UM], x[UM][EPL], mn = m;
+  const int b = blockIdx.y, r = W == 1 ? blockIdx.x * 4 + wave : blockIdx.x;
+  if (r >= a.rows) return;  // (W = 1)
+  const size_t row = (size_t)b * a.rows + r;
+  T* Y = reinterpret_cast<T*>(a.Y);
+  float* LSE = a.LSE;
+  const int start = W == 1 ? 0 : wave;
+  const float* own = a.part + (size_t)r * a.all * (D + 2);
+  int slot = b * a.splits, splits = a.pieces;
+  float mx[UM], lx[UM], x[UM][EPL];
+  const auto load = [&](int s0) {
 #pragma unroll
     for (int u = 0; u < UM; ++u) {
-      const int s = s0 + u * W;
-      const float* at = P + (size_t)min(s, splits - 1) * (D + 2);
+      const float* at = own + (size_t)(slot + min(s0 + u * W, splits - 1)) * (D + 2);
       mx[u] = at[D];
       lx[u] = at[D + 1];
 #pragma unroll
       for (int i = 0; i < EPL; ++i) x[u][i] = at[lane + 64 * i];
     }
+  };
+  load(start);
+  if (a.dealt) {  // (asked for beside the pieces that it usually says)
+    const int from = a.dealt[b], n = a.dealt[64 + b];
+    if (n == 1) return;  // written by the one piece
+    if (__builtin_expect(from != slot || n != splits, 0)) {
+      slot = from;
+      splits = n;
+      if (n > 0) load(start);
+    }
+  }
+  float m = -INFINITY, l = 0.f, o[EPL] = {};
+  for (int s0 = start; s0 < splits; s0 += W * UM) {
+    if (s0 > start) load(s0);
+    float mn = m;
 #pragma unroll
     for (int u = 0; u < UM; ++u) {
       if (s0 + u * W >= splits) {
@@ -838,14 +932,16 @@ Cache cache_of(const sa_cache4_desc* c, void* pool, const int32_t* table) {
   return k;
 }
 
-// How a call is dealt: the query rows of a KV head in `blocks` of 16 nt, the cache in `splits` pieces; `most`: what `splits` can be
+// How a call is dealt: the query rows of a KV head in `blocks` of 16 nt, the cache in `splits` pieces; `most`: what `slots` can be
 // for this many tiles or fewer (the workspace is sized for that).
 struct Plan {
   int nt;
-  long blocks, splits, most;
+  bool dealt;  // the sequences' pieces are dealt by their lengths if those differ much
+  long blocks, splits, slots, most;
 };
 constexpr int waves_of(int nt) { return nt == 1 ? 8 : 4; }
-Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
+constexpr int kDealtTo = 64;  // sequences, one a lane
+Plan pieces_plan(const sa_cache4_desc* c, int T, long tiles) {
   const long rows = (long)(c->Hq / c->Hkv) * T;
   Plan p;
   p.nt = rows <= 16 ? 1 : 2;
@@ -881,19 +977,34 @@ Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
   return p;
 }
 
+// Pieces of the longest sequence are `splits` equal ones; a sequence has `slots` workgroups.  Where a wave has 12 tiles or more and up to 64
+// sequences hold less than two thirds of the rows that as many longest ones would, the kernel deals the slots of all of them by their lengths (us,
+// bf16, 32 / 8 heads: 12 sequences of 1000 rows but one of 16384 24.4 -> 13.3; 500 to 7700 rows, B16 20.7 -> 19.4; even ones pay for the question, 16 of
+// 8192 rows 31.0 -> 31.3; of 3700 to 8192 rows, 73 %, 25.0 -> 25.8; with 5 tiles a wave, 20000 and 300 rows 12.1 -> 14.0).  A sequence that would be one
+// piece has a slot more for that from 16 tiles a wave on (31 of 600 rows and one of 12000 43.0 -> 15.6; 32 of 1000 to 4000 rows 20.2 as before).
+Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
+  Plan p = pieces_plan(c, T, tiles);
+  const long waves = waves_of(p.nt), each = (tiles + p.splits - 1) / p.splits;
+  const bool several = c->B > 1 && c->B <= kDealtTo;
+  p.slots = several && p.splits == 1 && p.nt == 1 && each >= 16 * waves ? 2 : p.splits;
+  p.dealt = several && p.slots > 1 && each >= 12 * waves;
+  if (p.most < p.slots) p.most = p.slots;
+  return p;
+}
+
 template <typename T, int D>
 hipError_t launch_attn(const sa_cache4_desc* c, AttnArgs& a, const Plan& p, hipStream_t st) {
   const long blocks = (long)c->B * c->Hkv * a.row_blocks * a.splits;
-  const long rows = (long)c->B * c->Hq * a.T;
+  const int rows = c->Hkv * a.rows;  // of a sequence
   if (!fits_a_launch(blocks, 512) || (a.splits > 1 && !fits_a_launch(rows, a.splits <= 16 ? 64 : 512))) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
   if (p.nt == 1) cache4_attn_kernel<T, D, 1, waves_of(1)><<<grid, 64 * waves_of(1), 0, st>>>(a);
   else cache4_attn_kernel<T, D, 2, waves_of(2)><<<grid, 64 * waves_of(2), 0, st>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.splits == 1) return e;
-  T* Y = reinterpret_cast<T*>(a.Y);
-  if (a.splits <= 16) cache4_merge_kernel<T, D, 1><<<(unsigned)((rows + 3) / 4), 256, 0, st>>>(a.part, Y, a.LSE, a.splits, (int)rows);
-  else cache4_merge_kernel<T, D, 8><<<(unsigned)rows, 512, 0, st>>>(a.part, Y, a.LSE, a.splits, (int)rows);
+  const MergeArgs m = {a.part, a.dealt, a.Y, a.LSE, rows, a.splits, a.pieces, c->B * a.splits};
+  if (a.splits <= 16) cache4_merge_kernel<T, D, 1><<<dim3((rows + 3) / 4, c->B), 256, 0, st>>>(m);
+  else cache4_merge_kernel<T, D, 8><<<dim3(rows, c->B), 512, 0, st>>>(m);
   return hipGetLastError();
 }
 
@@ -924,10 +1035,17 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
   return hipGetLastError();
 }
 
+constexpr size_t kDealtBytes = 2 * kDealtTo * sizeof(int32_t);
+
 size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T) {
   const long tiles = ((long)c->max_pages * c->page_rows) / kTile;
   const long splits = plan_of(c, T, tiles).most;
-  return splits <= 1 ? 0 : (size_t)c->B * c->Hq * T * (size_t)splits * (c->d + 2) * sizeof(float);
+  return splits <= 1 ? 0 : kDealtBytes + (size_t)c->B * c->Hq * T * (size_t)splits * (c->d + 2) * sizeof(float);
+}
+
+int cache4_decode_dealt(const sa_cache4_desc* c, int T, int max_len) {
+  const Plan p = plan_of(c, T, ((long)max_len + kTile - 1) / kTile);
+  return p.dealt ? (int)p.slots : 0;
 }
 
 int cache4_decode_plan(const sa_cache4_desc* c, int T, int max_len) {
@@ -939,13 +1057,17 @@ hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, c
                                 const int32_t* lens, int max_len, void* Y, float* LSE, void* ws, hipStream_t st) {
   AttnArgs a;
   a.c = cache_of(c, const_cast<void*>(pool), table);
-  a.q = q; a.Y = Y; a.LSE = LSE; a.part = reinterpret_cast<float*>(ws); a.lens = lens;
+  a.q = q; a.Y = Y; a.LSE = LSE; a.lens = lens;
   a.T = T; a.rows = (c->Hq / c->Hkv) * T; a.max_len = max_len;
   const long tiles = ((long)max_len + kTile - 1) / kTile;
   const Plan p = plan_of(c, T, tiles);
   a.row_blocks = (int)p.blocks;
   a.chunk = (int)((tiles + p.splits - 1) / p.splits);
-  a.splits = (int)((tiles + a.chunk - 1) / a.chunk);
+  a.pieces = (int)((tiles + a.chunk - 1) / a.chunk);
+  a.splits = p.slots > p.splits ? (int)p.slots : a.pieces;
+  a.part = reinterpret_cast<float*>(static_cast<char*>(ws) + kDealtBytes);
+  a.few = (uint32_t)(c->B * tiles * 2 / 3);
+  a.dealt = p.dealt && a.splits > 1 ? static_cast<int32_t*>(ws) : nullptr;
   a.scale_log2e = (c->scale > 0.f ? c->scale : 1.0f / sqrtf((float)c->d)) * kLog2e;
   if (c->dtype == SA_BF16) return c->d == 128 ? launch_attn<bf16_t, 128>(c, a, p, st) : launch_attn<bf16_t, 64>(c, a, p, st);
   return c->d == 128 ? launch_attn<float, 128>(c, a, p, st) : launch_attn<float, 64>(c, a, p, st);

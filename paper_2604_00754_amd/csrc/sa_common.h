@@ -117,6 +117,7 @@ size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T);
 hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, const void* pool, const int32_t* table,
                                 const int32_t* lens, int max_len, void* Y, float* LSE, void* ws, hipStream_t st);
 int cache4_decode_plan(const sa_cache4_desc* c, int T, int max_len);  // blocks of query rows a wave takes (1, 2) | pieces << 2
+int cache4_decode_dealt(const sa_cache4_desc* c, int T, int max_len);  // workgroups a sequence where the kernel may deal pieces by length, 0
 size_t pages_extend_workspace_bytes(const sa_cache4_desc* c);
 size_t pages_compact_workspace_bytes(const sa_cache4_desc* c);
 hipError_t launch_pages_fork(const sa_cache4_desc* c, const int32_t* parents, const int32_t* table, const int32_t* lens, const int32_t* refs,
@@ -165,6 +166,7 @@ const char* sa_internal_bwd_kernel(const sa_desc* desc, int permuted, int rotate
 const char* sa_internal_gate_kernel(const sa_desc* desc, int backward, int dual);
 // how sa_cache4_decode_fwd is dealt: cache4_decode_plan, 0 for what it refuses
 int sa_internal_cache4_plan(const sa_cache4_desc* desc, int T, int max_len);
+int sa_internal_cache4_dealt(const sa_cache4_desc* desc, int T, int max_len);
 // pieces of the tokens that add up to a 128 x 128 tile of dW in sa_gate_proj_bwd
 int sa_internal_gate_dw_pieces(const sa_desc* desc, int dual);
 // sa_sample_perm with room for `cap` keys of a bucket

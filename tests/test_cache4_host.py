@@ -161,6 +161,23 @@ def test_how_attention_is_dealt(B, Hq, Hkv, d, dtype, T, n, kernel, pieces):
     assert sa.cache4_plan(c, T, n) == (kernel, pieces)
 
 
+@pytest.mark.parametrize("B,Hq,Hkv,T,n,pieces,dealt", [
+    (1, 32, 8, 1, 32768, 32, 0),     # alone
+    (16, 32, 8, 1, 8192, 2, 2),
+    (12, 32, 8, 1, 16384, 3, 3),
+    (2, 32, 8, 1, 20000, 16, 0),     # few tiles a wave
+    (32, 32, 8, 1, 12000, 1, 2),     # a slot more
+    (32, 32, 8, 1, 4000, 1, 0),
+    (64, 32, 8, 1, 32768, 2, 2),
+    (65, 32, 8, 1, 32768, 2, 0),     # more sequences than lanes
+])
+def test_where_pieces_may_be_dealt_by_length(B, Hq, Hkv, T, n, pieces, dealt):
+    c = desc(B=B, Hq=Hq, Hkv=Hkv, d=128, max_pages=-(-n // 64), pages=100)
+    assert sa.cache4_plan(c, T, n) == (1, pieces) and sa.cache4_dealt(c, T, n) == dealt
+    if dealt:
+        assert sa.sa_cache4_workspace_bytes(c, sa.SA_OP_CACHE4_DECODE, T) >= 512 + B * Hq * T * dealt * 130 * 4
+
+
 def test_workspaces_cover_every_length():
     rng = np.random.default_rng(0)
     for _ in range(300):
@@ -173,6 +190,8 @@ def test_workspaces_cover_every_length():
             tiles, waves = -(-n // 32), 8 if kernel == 1 else 4
             assert pieces <= -(-tiles // waves) and -(-tiles // pieces) <= waves * (64 if kernel == 1 else 128)
             assert pieces == 1 or need >= c.B * c.Hq * T * pieces * (c.d + 2) * 4
+            slots = sa.cache4_dealt(c, T, n)
+            assert slots == 0 or slots >= pieces and need >= 512 + c.B * c.Hq * T * slots * (c.d + 2) * 4
 
 
 def test_outputs_that_overlap_inputs():

@@ -290,7 +290,12 @@ def test_values_of_any_size(dtype, d, sizes):
     (1, 8, 2, 128, "f32", 300, [6500], 2),
     (1, 8, 1, 64, "f32", 65, [20011], 2),
     (1, 32, 4, 128, "bf16", 1, [40001], 1),
-    (3, 12, 12, 64, "bf16", 1, [30000, 1, 777], 1),
+    (3, 12, 12, 64, "bf16", 1, [30000, 1, 777], 1),                  # pieces dealt by length, as in those below
+    (12, 32, 8, 128, "bf16", 1, [1000] * 5 + [16384] + [1001] * 6, 1),
+    (32, 32, 8, 128, "bf16", 1, [600] * 31 + [12000], 1),            # sequences of one piece beside others
+    (64, 4, 1, 64, "f32", 1, [40] * 20 + [14000] + [33] * 43, 1),
+    (9, 32, 8, 128, "bf16", 6, [7, 12000, 6, 3001, 64, 9, 100, 5, 700], 2),
+    (5, 8, 4, 64, "f32", 40, [30, 8192, 41, 3001, 64], 2),
 ])
 def test_many_rows(B, Hq, Hkv, d, dtype, T, lens, kernel):
     """Long caches and many tokens against fp64 on the rows as they are read back; some elements of q 60 times as large as others, some a
@@ -362,6 +367,45 @@ def test_a_sequence_does_not_depend_on_the_others():
         _, Y2, L2 = c.decode(1, lens, bound, q=q)
         assert np.abs(Y2[0] - Y[0]).max() <= 2.0 ** -7 * np.abs(Y[0]).max()
     assert np.array_equal(Y2, Y) and np.array_equal(L2, L)
+
+
+@pytest.mark.parametrize("B,Hq,Hkv,d,dtype,T", [(64, 4, 2, 64, "bf16", 1), (33, 32, 8, 128, "bf16", 1), (7, 40, 8, 64, "f32", 5)])
+def test_lengths_far_below_their_bound(B, Hq, Hkv, d, dtype, T):
+    """Pieces dealt by length, empty sequences and lengths out of range among them, pages missing: as calls for each sequence alone, and the
+    same bits twice"""
+    n, R = 8192, 64
+    c = Setup(B, Hq, Hkv, d, R, n // R, dtype, seed=B)
+    assert sa().cache4_dealt(c.desc, T, n) > 0
+    g = torch.Generator(device=U.DEV).manual_seed(B)
+    lens = c.rng.integers(0, 300, B)
+    lens[[0, 2, B - 1]], lens[1], lens[3], lens[4] = 0, 10 ** 9, -5, 5000
+    c.table[1, 7] = -1
+    table = c.dev(c.table)
+    # any codes, with scales of 2^-2 .. 2: what is held is up to 12
+    c.pool.copy_(torch.randint(0, 256, c.pool.shape, device=U.DEV, generator=g, dtype=torch.uint8))
+    tiles = c.pool.view(-1, 34 * d)
+    tiles[:, 32 * d:] = 125 + tiles[:, 32 * d:] % 4
+    q = torch.randn(B, Hq, T, d, device=U.DEV, generator=g).to(U.tdtype(dtype))
+    _, Y, L = c.decode(T, lens.tolist(), n, q=q)
+    _, Y2, L2 = c.decode(T, lens.tolist(), n, q=q)
+    assert np.array_equal(Y, Y2) and np.array_equal(L, L2)
+    one = sa().make_cache4_desc(1, Hq, Hkv, d, R, c.P, n // R, 1, c.desc.dtype, 0.0)
+    ws = torch.empty(max(16, sa().sa_cache4_workspace_bytes(one, sa().SA_OP_CACHE4_DECODE, T)), dtype=torch.uint8, device=U.DEV)
+    assert sa().cache4_dealt(one, T, n) == 0
+    for b in range(B):
+        y, l = torch.empty_like(q[b:b + 1]), torch.empty(1, Hq, T, device=U.DEV)
+        sa().sa_cache4_decode_fwd(one, q[b:b + 1].contiguous(), c.pool, table[b:b + 1].contiguous(), c.dev(lens[b:b + 1].astype(np.int32)), n, y, l, ws)
+        y, l = U.to_np64(y)[0], l[0].cpu().numpy().astype(np.float64)
+        m = min(max(int(lens[b]), 0), n)
+        assert np.array_equal(np.isneginf(l), np.isneginf(L[b])) and np.isneginf(l).any() == (m < T or m == 0)
+        assert (Y[b][np.isneginf(l)] == 0).all()
+        # both sides: probabilities of 11 bits (fp32: 22 or more) and sums of m rows cut differently, values up to 6 * 2; scores and LSE are
+        # sums of the same products in the same order, exponentials of arguments up to 128 rounded to 2^-24 of themselves
+        p, half = (2.0 ** -12, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -23, 2.0 ** -24)
+        tol = 2 * half * np.abs(y) + 2 * 12 * (p + 2 * m * 2.0 ** -24 + 2.0 ** -16)
+        assert (np.abs(Y[b] - y) <= tol).all(), (b, np.abs(Y[b] - y).max())
+        fine = np.isfinite(l)
+        assert (np.abs(L[b][fine] - l[fine]) <= 2 * m * 2.0 ** -24 + 2.0 ** -16).all()
 
 
 def test_decode_continues_a_prompt_pass():
