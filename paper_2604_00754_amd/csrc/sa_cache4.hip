@@ -982,10 +982,12 @@ Plan pieces_plan(const sa_cache4_desc* c, int T, long tiles) {
 // bf16, 32 / 8 heads: 12 sequences of 1000 rows but one of 16384 24.4 -> 13.3; 500 to 7700 rows, B16 20.7 -> 19.4; even ones pay for the question, 16 of
 // 8192 rows 31.0 -> 31.3; of 3700 to 8192 rows, 73 %, 25.0 -> 25.8; with 5 tiles a wave, 20000 and 300 rows 12.1 -> 14.0).  A sequence that would be one
 // piece has a slot more for that from 16 tiles a wave on (31 of 600 rows and one of 12000 43.0 -> 15.6; 32 of 1000 to 4000 rows 20.2 as before).
+// More than one block of query rows makes workgroups enough that the short ones' places are taken by others (the first batch, 6 tokens 28.8 -> 21.3,
+// 16 tokens in two blocks 37.4 -> 38.3).
 Plan plan_of(const sa_cache4_desc* c, int T, long tiles) {
   Plan p = pieces_plan(c, T, tiles);
   const long waves = waves_of(p.nt), each = (tiles + p.splits - 1) / p.splits;
-  const bool several = c->B > 1 && c->B <= kDealtTo;
+  const bool several = c->B > 1 && c->B <= kDealtTo && p.blocks == 1;
   p.slots = several && p.splits == 1 && p.nt == 1 && each >= 16 * waves ? 2 : p.splits;
   p.dealt = several && p.slots > 1 && each >= 12 * waves;
   if (p.most < p.slots) p.most = p.slots;

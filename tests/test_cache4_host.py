@@ -170,10 +170,12 @@ def test_how_attention_is_dealt(B, Hq, Hkv, d, dtype, T, n, kernel, pieces):
     (32, 32, 8, 1, 4000, 1, 0),
     (64, 32, 8, 1, 32768, 2, 2),
     (65, 32, 8, 1, 32768, 2, 0),     # more sequences than lanes
+    (12, 32, 8, 6, 16384, 5, 5),
+    (12, 32, 8, 16, 16384, 5, 0),    # two blocks of query rows
 ])
 def test_where_pieces_may_be_dealt_by_length(B, Hq, Hkv, T, n, pieces, dealt):
     c = desc(B=B, Hq=Hq, Hkv=Hkv, d=128, max_pages=-(-n // 64), pages=100)
-    assert sa.cache4_plan(c, T, n) == (1, pieces) and sa.cache4_dealt(c, T, n) == dealt
+    assert sa.cache4_plan(c, T, n) == (1 if T == 1 else 2, pieces) and sa.cache4_dealt(c, T, n) == dealt
     if dealt:
         assert sa.sa_cache4_workspace_bytes(c, sa.SA_OP_CACHE4_DECODE, T) >= 512 + B * Hq * T * dealt * 130 * 4
 

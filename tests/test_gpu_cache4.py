@@ -295,7 +295,7 @@ def test_values_of_any_size(dtype, d, sizes):
     (32, 32, 8, 128, "bf16", 1, [600] * 31 + [12000], 1),            # sequences of one piece beside others
     (64, 4, 1, 64, "f32", 1, [40] * 20 + [14000] + [33] * 43, 1),
     (9, 32, 8, 128, "bf16", 6, [7, 12000, 6, 3001, 64, 9, 100, 5, 700], 2),
-    (5, 8, 4, 64, "f32", 40, [30, 8192, 41, 3001, 64], 2),
+    (40, 8, 4, 64, "f32", 16, [30, 8192] + [41] * 37 + [3001], 2),
 ])
 def test_many_rows(B, Hq, Hkv, d, dtype, T, lens, kernel):
     """Long caches and many tokens against fp64 on the rows as they are read back; some elements of q 60 times as large as others, some a
