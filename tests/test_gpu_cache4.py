@@ -408,6 +408,35 @@ def test_lengths_far_below_their_bound(B, Hq, Hkv, d, dtype, T):
         assert (np.abs(L[b][fine] - l[fine]) <= 2 * m * 2.0 ** -24 + 2.0 ** -16).all()
 
 
+def test_replays_deal_the_pieces_of_their_own_lengths():
+    """One recorded call, even lengths and very different ones in turn, each replay against an eager call with a workspace of its own"""
+    B, Hq, Hkv, d, n = 16, 16, 4, 64, 16384
+    c = Setup(B, Hq, Hkv, d, 64, n // 64, "bf16", seed=3)
+    assert sa().cache4_dealt(c.desc, 1, n) > 0
+    g = torch.Generator(device=U.DEV).manual_seed(3)
+    c.pool.copy_(torch.randint(0, 256, c.pool.shape, device=U.DEV, generator=g, dtype=torch.uint8))
+    tiles = c.pool.view(-1, 34 * d)
+    tiles[:, 32 * d:] = 125 + tiles[:, 32 * d:] % 4
+    q = torch.randn(B, Hq, 1, d, device=U.DEV, generator=g).to(torch.bfloat16)
+    lens, table = torch.full((B,), n, dtype=torch.int32, device=U.DEV), c.dev(c.table)
+    need = sa().sa_cache4_workspace_bytes(c.desc, sa().SA_OP_CACHE4_DECODE, 1)
+    ws, ws2 = (torch.empty(need, dtype=torch.uint8, device=U.DEV) for _ in range(2))
+    Y, Y2 = torch.empty_like(q), torch.empty_like(q)
+    L, L2 = (torch.empty(B, Hq, 1, device=U.DEV) for _ in range(2))
+    sa().sa_cache4_decode_fwd(c.desc, q, c.pool, table, lens, n, Y, L, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sa().sa_cache4_decode_fwd(c.desc, q, c.pool, table, lens, n, Y, L, ws)
+    for k, rows in enumerate(([n] * B, [100] * 15 + [n], [0] * 16, [n, 1] * 8, [900 * i for i in range(16)], [n] * B)):
+        lens.copy_(torch.tensor(rows, dtype=torch.int32))
+        ws2.fill_(255)
+        graph.replay()
+        sa().sa_cache4_decode_fwd(c.desc, q, c.pool, table, lens, n, Y2, L2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(Y, Y2) and torch.equal(L, L2) and torch.isfinite(Y).all(), k
+
+
 def test_decode_continues_a_prompt_pass():
     """Attention over rows written and read back equals the framework's dense decoding step on the rows as read."""
     B, Hq, Hkv, d, n = 2, 8, 2, 128, 700
