@@ -120,6 +120,8 @@ def _load():
     lib.sa_internal_cache4_plan.argtypes = [cp, C.c_int, C.c_int]
     lib.sa_internal_cache4_dealt.restype = C.c_int
     lib.sa_internal_cache4_dealt.argtypes = [cp, C.c_int, C.c_int]
+    lib.sa_internal_cache4_loaded_rows.restype = C.c_int
+    lib.sa_internal_cache4_loaded_rows.argtypes = [C.c_int32, C.c_int32, C.c_int32, C.c_int, ip]
     lib.sa_internal_gate_dw_pieces.restype = C.c_int
     lib.sa_internal_gate_dw_pieces.argtypes = [dp, C.c_int]
     lib.swa_fwd.restype = C.c_int
@@ -363,6 +365,14 @@ def cache4_dealt(desc, T, max_len):
     """Workgroups of a sequence (for each KV head and block of query rows) where sa_cache4_decode_fwd deals all of them by the sequences'
     lengths if those differ much, else 0."""
     return _lib.sa_internal_cache4_dealt(C.byref(desc), int(T), int(max_len))
+
+
+def cache4_loaded_rows(start, count, T):
+    """For every half tile that sa_cache4_write looks at: the 16 rows of K and V that it loads there, or None."""
+    out, rows = [], (C.c_int32 * 16)()
+    while (there := _lib.sa_internal_cache4_loaded_rows(start, count, T, len(out), rows)) >= 0:
+        out.append(list(rows) if there else None)
+    return out
 
 
 def raw():

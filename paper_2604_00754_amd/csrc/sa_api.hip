@@ -725,6 +725,10 @@ int sa_internal_cache4_dealt(const sa_cache4_desc* c, int T, int max_len) {
   return sa::cache4_decode_dealt(c, T, max_len);
 }
 
+int sa_internal_cache4_loaded_rows(int32_t start, int32_t count, int32_t T, int half, int32_t* rows) {
+  return T < 1 || !rows ? -1 : sa::cache4_loaded_rows(start, count, T, half, rows);
+}
+
 sa_status sa_pages_fork(const sa_cache4_desc* c, const int32_t* parents, const int32_t* table, const int32_t* lens,
                         const int32_t* refs, int32_t* table_out, int32_t* lens_out, int32_t* refs_out, void* stream) {
   sa_status s = validate_cache4(c);

@@ -152,6 +152,19 @@ struct Rows {
   bool any, whole;        // whether rows of the half are among those asked for, and all
 };
 constexpr int kRowWaves = 4;
+// Half k of those that the rows starts .. can touch; plain arithmetic, which the host's tests go through as well.
+struct HalfRows { long tile, t0; bool any; };
+__host__ __device__ __forceinline__ HalfRows half_rows(int start, int count, int tiles, int k) {
+  HalfRows h;
+  h.tile = (long)(start >> 5) + (k >> 1);
+  h.t0 = h.tile * kTile + 16 * (k & 1) - start;
+  h.any = count > 0 && k < 2 * tiles && h.t0 < count && h.t0 + 16 > 0;  // (no rows: also where the first tile is a begun one)
+  return h;
+}
+// The row that is loaded for t: where t is not written, the first or last (of at least one) in its place.
+__host__ __device__ __forceinline__ long loaded_row(long t, int count) { return t < 0 ? 0 : t < count ? t : count - 1; }
+__host__ __device__ __forceinline__ int tiles_touched(int T) { return (int)(((long)T + 62) / kTile); }  // the first and the last may be begun
+
 __device__ __forceinline__ Rows rows_of_wave(const RowsArgs& a) {
   Rows w;
   const unsigned blocks = (unsigned)(2 * a.tiles + kRowWaves - 1) / kRowWaves, bh = blockIdx.x / blocks;
@@ -161,11 +174,11 @@ __device__ __forceinline__ Rows rows_of_wave(const RowsArgs& a) {
   w.half = k & 1;
   const int start = a.starts ? __builtin_amdgcn_readfirstlane(a.starts[w.b]) : 0;
   w.count = a.counts ? __builtin_amdgcn_readfirstlane(min(max(a.counts[w.b], 0), a.T)) : a.T;
-  const long tile = (long)(start >> 5) + (k >> 1);
-  w.t0 = tile * kTile + 16 * w.half - start;
-  w.any = k < 2 * a.tiles && w.t0 < w.count && w.t0 + 16 > 0;
+  const HalfRows h = half_rows(start, w.count, a.tiles, k);
+  w.t0 = h.t0;
+  w.any = h.any;
   w.whole = w.t0 >= 0 && w.t0 + 16 <= w.count;
-  w.tile = tile < 0 || tile * kTile >= a.c.capacity ? -1 : (int)tile;
+  w.tile = h.tile < 0 || h.tile * kTile >= a.c.capacity ? -1 : (int)h.tile;
   return w;
 }
 
@@ -186,10 +199,10 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_write_kernel(RowsArgs a
   const T* kr = reinterpret_cast<const T*>(a.K) + src * D + r * E;
   const T* vr = reinterpret_cast<const T*>(a.V) + src * D + r * E;
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {  // (rows that are not written: the first or last that is in their place)
+  for (int j = 0; j < 4; ++j) {
     const long t = w.t0 + 4 * g + j;
     in[j] = t >= 0 && t < w.count;
-    const size_t at = (size_t)(t < 0 ? 0 : t < w.count ? t : w.count - 1) * D;
+    const size_t at = (size_t)loaded_row(t, w.count) * D;
     k[j].load(kr + at);
     v[j].load(vr + at);
   }
@@ -1017,7 +1030,7 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
   RowsArgs a;
   a.c = cache_of(c, pool, table);
   a.starts = starts; a.counts = counts; a.K = K; a.V = V; a.T = T;
-  a.tiles = (int)(((long)T + 62) / kTile);  // the first and the last may be begun
+  a.tiles = tiles_touched(T);
   const long blocks = (long)c->B * c->Hkv * ((2 * (long)a.tiles + kRowWaves - 1) / kRowWaves);
   if (!fits_a_launch(blocks, kRowWaves * 64)) return hipErrorNotSupported;
   const unsigned grid = (unsigned)blocks;
@@ -1035,6 +1048,14 @@ hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void
     else cache4_read_kernel<float, 64><<<grid, block, 0, st>>>(a);
   }
   return hipGetLastError();
+}
+
+int cache4_loaded_rows(int start, int count, int T, int half, int32_t* rows) {
+  if (half < 0 || half >= 2 * tiles_touched(T)) return -1;
+  count = count < 0 ? 0 : count > T ? T : count;
+  const HalfRows h = half_rows(start, count, tiles_touched(T), half);
+  for (int j = 0; j < 16 && h.any; ++j) rows[j] = (int32_t)loaded_row(h.t0 + j, count);
+  return h.any ? 1 : 0;
 }
 
 constexpr size_t kDealtBytes = 2 * kDealtTo * sizeof(int32_t);

@@ -113,6 +113,7 @@ hipError_t launch_decode(const Decode& d, hipStream_t st);
 // sa_cache4.hip, sa_pages.hip: caches in 4 bits and in pages.  K, V of the rows: written, or (write = false) read back into
 hipError_t launch_cache4_rows(const sa_cache4_desc* c, bool write, void* K, void* V, int T, const int32_t* starts,
                               const int32_t* counts, const int32_t* table, void* pool, hipStream_t st);
+int cache4_loaded_rows(int start, int count, int T, int half, int32_t* rows);
 size_t cache4_decode_workspace_bytes(const sa_cache4_desc* c, int T);
 hipError_t launch_cache4_decode(const sa_cache4_desc* c, const void* q, int T, const void* pool, const int32_t* table,
                                 const int32_t* lens, int max_len, void* Y, float* LSE, void* ws, hipStream_t st);
@@ -167,6 +168,9 @@ const char* sa_internal_gate_kernel(const sa_desc* desc, int backward, int dual)
 // how sa_cache4_decode_fwd is dealt: cache4_decode_plan, 0 for what it refuses
 int sa_internal_cache4_plan(const sa_cache4_desc* desc, int T, int max_len);
 int sa_internal_cache4_dealt(const sa_cache4_desc* desc, int T, int max_len);
+// the 16 rows of K and V that sa_cache4_write loads for a half of a tile (counted from the one that holds the first position): 1, 0 if it
+// loads none there, -1 past the last half that is looked at
+int sa_internal_cache4_loaded_rows(int32_t start, int32_t count, int32_t T, int half, int32_t* rows);
 // pieces of the tokens that add up to a 128 x 128 tile of dW in sa_gate_proj_bwd
 int sa_internal_gate_dw_pieces(const sa_desc* desc, int dual);
 // sa_sample_perm with room for `cap` keys of a bucket

@@ -196,6 +196,19 @@ def test_workspaces_cover_every_length():
             assert slots == 0 or slots >= pieces and need >= 512 + c.B * c.Hq * T * slots * (c.d + 2) * 4
 
 
+@pytest.mark.parametrize("T", [1, 2, 15, 16, 17, 33, 40])
+def test_rows_that_are_loaded_are_rows_that_are_written(T):
+    """Whatever start and count are: no row in front of the sequence's or past its count is touched, a sequence without rows touches none"""
+    for start in [*range(64), -1, -20, -32, -33, 2 ** 31 - 1, -(2 ** 31)]:
+        for count in [*range(T + 1), -1, -(2 ** 31), T + 1, 2 ** 31 - 1]:
+            rows = min(max(count, 0), T)
+            seen = set()
+            for half in sa.cache4_loaded_rows(start, count, T):
+                assert half is None or 0 <= min(half) and max(half) < rows, (start, count, half)
+                seen.update(half or ())
+            assert seen == set(range(rows)), (start, count)
+
+
 def test_outputs_that_overlap_inputs():
     d = desc()
     name = "sa_pages_fork"
