@@ -377,8 +377,8 @@ struct MergeArgs {
 
 // The maximum is raised where a score passes it by more than 2^kRaise: the usual tile needs no exchange between lanes and no product with a
 // correction.  With the lift the largest probability is 2^15, a row's own largest at least 2^7, and f16 holds all its bits down to 2^-14.
-// kNone: the maximum before a row has been seen, a finite number (a row that is not seen has the score -inf).
-constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.0e38f;
+// kNone: the maximum before a row has been seen, the lowest number (a row that is not seen has the score -inf).
+constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.402823466e38f;
 
 __device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
 
@@ -553,15 +553,19 @@ __device__ __forceinline__ void load_queries(const T* q, int row0, int rows, int
 }
 
 // Scores of 8 rows -> probabilities relative to the running maximum m (log2 domain, 2^kLift above it), their sum added to l.  They are
-// formed with the maximum at hand; where one is past 2^(kLift + kRaise), the maximum is raised and l and o are brought to the new one.
+// formed with the maximum at hand; where one is past 2^(kLift + kRaise), the maximum is raised and l and o are brought to the new one.  Then
+// products are rounded before the maximum is taken off, as in the maximum itself: the largest is 2^kLift whatever the scores' size, where a
+// fused product would differ by half a unit of the maximum's last place (from scores of 2^28 on, more than f16 holds).
 template <int D>
 __device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, float& l, f32x4* o) {
-  float e[8], ref = kLift - m;
+  float e[8];
+  const float ref = kLift - m;
 #pragma unroll
   for (int j = 0; j < 8; ++j) e[j] = fmaf(p[j], scale_log2e, ref);
   float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), e[2]), fmaxf(fmaxf(e[3], e[4]), e[5]));
   top = fmaxf(fmaxf(top, e[6]), e[7]);
   if (__any(top > kLift + kRaise)) {
+#pragma clang fp contract(off)
     float mn = p[0];
 #pragma unroll
     for (int j = 1; j < 8; ++j) mn = fmaxf(mn, p[j]);
@@ -572,9 +576,8 @@ __device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, flo
 #pragma unroll
     for (int d = 0; d < D / 16; ++d) o[d] *= corr;
     m = mn;
-    ref = kLift - m;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = fmaf(p[j], scale_log2e, ref);
+    for (int j = 0; j < 8; ++j) e[j] = p[j] * scale_log2e - m + kLift;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
