@@ -376,7 +376,8 @@ struct MergeArgs {
 };
 
 // The maximum is raised where a score passes it by more than 2^kRaise: the usual tile needs no exchange between lanes and no product with a
-// correction.  With the lift the largest probability is 2^15, a row's own largest at least 2^7, and f16 holds all its bits down to 2^-14.
+// correction.  With the lift the largest probability is 2^15, a row's own largest at least 2^7, and f16 holds all its bits down to 2^-14.  Over
+// values of V past f16's reach the lift is lowered (bf16_lift), so that no sum overflows.
 // kNone: the maximum before a row has been seen, the lowest number (a row that is not seen has the score -inf).
 constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.402823466e38f;
 
@@ -552,19 +553,26 @@ __device__ __forceinline__ void load_queries(const T* q, int row0, int rows, int
   }
 }
 
-// Scores of 8 rows -> probabilities relative to the running maximum m (log2 domain, 2^kLift above it), their sum added to l.  They are
-// formed with the maximum at hand; where one is past 2^(kLift + kRaise), the maximum is raised and l and o are brought to the new one.  Then
-// products are rounded before the maximum is taken off, as in the maximum itself: the largest is 2^kLift whatever the scores' size, where a
+// Lift of the probabilities over rows of V whose largest scale byte is `byte`, of a sequence of len rows: a probability is at most 2^(lift + kRaise), a
+// value below 2^(byte - 124), so that all of them together stay below 2^127.
+__device__ __forceinline__ float bf16_lift(int byte, int len) {
+  const int rows_log2 = 32 - __builtin_clz(((unsigned)max(len, 1) - 1u) | 1u);
+  return fminf(kLift, (float)(127 + 124 - (int)kRaise - byte - rows_log2));
+}
+
+// Scores of 8 rows -> probabilities relative to the running maximum m (log2 domain, 2^lift above it), their sum added to l.  They are
+// formed with the maximum at hand; where one is past 2^(lift + kRaise), the maximum is raised and l and o are brought to the new one.  Then
+// products are rounded before the maximum is taken off, as in the maximum itself: the largest is 2^lift whatever the scores' size, where a
 // fused product would differ by half a unit of the maximum's last place (from scores of 2^28 on, more than f16 holds).
 template <int D>
-__device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, float& l, f32x4* o) {
+__device__ __forceinline__ void weigh(float* p, float scale_log2e, float lift, float& m, float& l, f32x4* o) {
   float e[8];
-  const float ref = kLift - m;
+  const float ref = lift - m;
 #pragma unroll
   for (int j = 0; j < 8; ++j) e[j] = fmaf(p[j], scale_log2e, ref);
   float top = fmaxf(fmaxf(fmaxf(e[0], e[1]), e[2]), fmaxf(fmaxf(e[3], e[4]), e[5]));
   top = fmaxf(fmaxf(top, e[6]), e[7]);
-  if (__any(top > kLift + kRaise)) {
+  if (__any(top > lift + kRaise)) {
 #pragma clang fp contract(off)
     float mn = p[0];
 #pragma unroll
@@ -577,7 +585,7 @@ __device__ __forceinline__ void weigh(float* p, float scale_log2e, float& m, flo
     for (int d = 0; d < D / 16; ++d) o[d] *= corr;
     m = mn;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = p[j] * scale_log2e - m + kLift;
+    for (int j = 0; j < 8; ++j) e[j] = p[j] * scale_log2e - m + lift;
   }
 #pragma unroll
   for (int j = 0; j < 8; ++j) {
@@ -712,10 +720,16 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
   f32x4 o[NT][DB];
   float m[NT], l[NT];
   const int turns = max(0, (min(end, most < 0 ? 0 : most / kTile + 1) - first + W - 1) / W);
+  auto place = [&](int i) {  // (a tile that is not there: the first of the pool in its place, not seen)
+    const int number = number_of(i);
+    return __builtin_amdgcn_make_buffer_rsrc(a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes, 0, L::kBytes, 0x20000);
+  };
+  float lift = kLift;
   // The wave's tiles, with V as operands of the type of `kind`; false if a tile's scales are out of f16's reach.
   auto walk = [&](auto kind) -> bool {
     using Operand = decltype(kind);
     constexpr bool kHalf = __is_same(Operand, f16x8);
+    const float up = kHalf ? kLift : lift;
     uint32_t unfit = 0;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
@@ -725,10 +739,6 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
       l[n] = 0.f;
     }
     TileRegs<D> x;
-    auto place = [&](int i) {  // (a tile that is not there: the first of the pool in its place, not seen)
-      const int number = number_of(i);
-      return __builtin_amdgcn_make_buffer_rsrc(a.c.pool + (size_t)(number < 0 ? 0 : number) * L::kBytes, 0, L::kBytes, 0x20000);
-    };
     x.place(r, g);
     if (turns == 0) return true;
     x.load_k(place(0));
@@ -778,7 +788,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
         unfit |= off & 0xe0e0e0e0u;
       }
 #pragma unroll
-      for (int n = 0; n < NT; ++n) weigh<D>(p[n], a.scale_log2e, m[n], l[n], o[n]);
+      for (int n = 0; n < NT; ++n) weigh<D>(p[n], a.scale_log2e, up, m[n], l[n], o[n]);
       __builtin_amdgcn_sched_barrier(0);
       float vscale[8];
 #pragma unroll
@@ -790,9 +800,25 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     }
     return !__any(unfit != 0);
   };
-  if (!walk(f16x8{})) walk(bf16x8{});
+  if (!walk(f16x8{})) {
+    // the largest scale of V in the tiles: a lane's eight are those of rows 4 g .. of both halves
+    int byte = 0;
+    const int at = L::kVs + ((r / L::LPB) * 4 + g) * 8;
+#pragma unroll 1
+    for (int i = 0; i < turns; ++i) {
+      const int rows = number_of(i) < 0 ? 0 : len - (first + W * i) * kTile - 4 * g;  // rows that are there from 4 g on
+      const u32x2 vs = __builtin_amdgcn_raw_buffer_load_b64(place(i), at, 0, 0);
 #pragma unroll
-  for (int n = 0; n < NT; ++n) m[n] -= kLift;  // what the sums are relative to
+      for (int j = 0; j < 8; ++j) byte = L::row(0, j) < rows ? max(byte, (int)((vs[j / 4] >> (8 * (j & 3))) & 0xffu)) : byte;
+    }
+    int most_byte = 0;  // the wave's, bit by bit (exchanged between lanes it costs registers that the walk needs)
+#pragma unroll
+    for (int bit = 128; bit > 0; bit >>= 1) most_byte |= __any(byte >= (most_byte | bit)) ? bit : 0;
+    lift = bf16_lift(most_byte, len);
+    walk(bf16x8{});
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n] -= lift;  // what the sums are relative to
 
   // the waves' results, 16 query rows at a time
 #pragma unroll

@@ -15,6 +15,60 @@ def held(c, x):
     return t, U.to_np64(t)
 
 
+# ---- V ------------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("sizes", [(2.0 ** 109, 1.0), (2.0 ** 112, 2.0 ** 112), (2.0 ** 119, 2.0 ** 3), (2.0 ** 124, 2.0 ** 124), (2.0 ** 124, 2.0 ** -100)])
+def test_large_values_of_v(dtype, d, sizes):
+    """Both signs, the sizes in turn from tile to tile; one row, few, several tiles a wave"""
+    c = Setup(1, 4, 1, d, 32, 9, dtype, seed=d)
+    K = c.rows(288)
+    V = c.rng.uniform(0.5, 1.5, (1, 1, 288, d)).astype(np.float32) * c.rng.choice([-1, 1], (1, 1, 288, d))
+    V *= np.repeat(np.resize(np.float32(sizes), 9), 32)[:, None]
+    c.write(K, held(c, V))
+    for T, n in ((1, 1), (1, 20), (1, 288), (3, 2), (20, 288)):
+        c.check(T, [n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_values_of_v_come_back_finite(dtype, d):
+    """6 * 2^125 in all rows: the mean is that, however many there are.  Weights enter product and sum alike; the two are kept to n 2^-24 each, a
+    weight's parts in the product to 2^-16 (bf16) and 2^-23 (fp32: three parts), and the quotient is rounded."""
+    top = 6 * 2.0 ** 125
+    for T, n in ((1, 1), (1, 33), (1, 20000), (20, 1500)):
+        c = Setup(1, 4, 1, d, 64, -(-n // 64), dtype, seed=n)
+        K = c.rows(n)[0]
+        V = torch.full_like(K, top)
+        V[..., 1::2] = -top
+        sa().sa_cache4_write(c.desc, K, V, None, None, c.dev(c.table), c.pool)
+        _, Y, L = c.decode(T, [n])
+        want = V[0, 0, 0].double().cpu().numpy()
+        parts, half = (2.0 ** -16, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -23, 2.0 ** -24)
+        assert np.isfinite(L).all() and (np.abs(Y / want - 1) <= half + parts + 2 * n * 2.0 ** -24).all(), (T, n, np.abs(Y / want - 1).max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_large_values_of_v_and_scores_that_rise(dtype):
+    """The maximum is raised over sums that are large already; large rows that no query sees (behind the last, on a page that is not there)"""
+    c = Setup(2, 4, 1, 64, 32, 12, dtype, seed=4, scale=0.5)
+    K = c.rows(384)[0]
+    K = (K.float() * torch.linspace(0.05, 12, 384, device=U.DEV)[:, None]).to(K.dtype)
+    V = c.rows(384)[0]
+    V[:, :, :64] *= 2.0 ** 124
+    V[1, :, 64:] *= 2.0 ** 60
+    V = V.clamp(-2.0 ** 126, 2.0 ** 126)
+    c.write((K, U.to_np64(K)), (V, U.to_np64(V)))
+    c.check(3, [384, 384])
+    c.check(1, [100, 33])
+    table = c.table.copy()
+    table[0, :2] = -1
+    q, Y, L = c.decode(3, [384, 384], table=table)
+    assert np.abs(Y[0]).max() < 10 and np.isfinite(Y).all() and np.isfinite(L).all()
+
+
 # ---- scores -------------------------------------------------------------------------------------------------------------------
 
 
