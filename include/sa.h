@@ -337,7 +337,7 @@ sa_status sa_cache4_read(const sa_cache4_desc* desc, const void* pool, const int
  * more: drafted tokens, a follow-up prompt).  q, Y [B,Hq,T,d], LSE [B,Hq,T] (fp32, may be NULL).  lens [B] (int32,
  * device): rows of each sequence, the T tokens' own included, clamped to 0..max_len on the device; max_len (host,
  * 1 <= max_len <= max_pages*page_rows) sizes the launch.  Token t sees the positions <= lens[b] - T + t whose pages are there;
- * one that sees none gets Y = 0 and LSE = -inf.  B*Hq*T < 2^31 (SA_ERR_SHAPE).
+ * one that sees none gets Y = 0 and LSE = -inf, one whose scores are all -inf (in fp32) NaN in both.  B*Hq*T < 2^31 (SA_ERR_SHAPE).
  * Scores, softmax and sums are fp32; q, K and V enter exactly, probabilities with 11 bits (bf16) or 22 (fp32) or more.
  * Where the sums are cut depends on the sizes and, in a batch, on all of its lengths: a sequence's results agree between batches to
  * the rounding above, between equal calls to the bit.

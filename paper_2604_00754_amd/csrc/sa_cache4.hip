@@ -381,6 +381,12 @@ struct MergeArgs {
 // kNone: the maximum before a row has been seen, the lowest number (a row that is not seen has the score -inf).
 constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.402823466e38f;
 
+// A query's sum of weights is 0 where it sees nothing and at least 2^-50 where it sees a number; kAllBelow and its multiples stand for rows whose scores
+// are all -inf, beside which any number counts alone and whose own softmax is 0/0.
+constexpr float kAllBelow = 0x1p-126f, kSomething = 0x1p-100f;
+__device__ __forceinline__ float weighted_mean(float v, float sum) { return sum == 0.f ? 0.f : sum < kSomething ? __uint_as_float(0x7fc00000u) : v / sum; }
+__device__ __forceinline__ float log_of_sum(float m, float sum) { return sum == 0.f ? -INFINITY : sum < kSomething ? __uint_as_float(0x7fc00000u) : (m + log2f(sum)) * kLn2; }
+
 __device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
@@ -826,6 +832,12 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     float ls = l[n];
     ls += __shfl_xor(ls, 16);
     ls += __shfl_xor(ls, 32);
+    if (__any(ls == 0.f && last[n] >= first * kTile)) {  // pages that are not there, or scores that are all -inf
+      bool seen = false;
+#pragma unroll 1
+      for (int i = 0; i < turns; ++i) seen |= number_of(i) >= 0 && (first + W * i) * kTile <= last[n];
+      if (ls == 0.f && seen) ls = kAllBelow;
+    }
     if (n > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -853,8 +865,8 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
       }
       const size_t out = (size_t)bh * a.rows + row;
       if (pieces == 1) {
-        store_y(reinterpret_cast<T*>(a.Y) + out * D + e, sum == 0.f ? 0.f : v / sum);
-        if (e == 0 && a.LSE) a.LSE[out] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+        store_y(reinterpret_cast<T*>(a.Y) + out * D + e, weighted_mean(v, sum));
+        if (e == 0 && a.LSE) a.LSE[out] = log_of_sum(M, sum);
       } else {
         float* to = a.part + (((size_t)hk * a.rows + row) * (a.c.B * a.splits) + slot) * (D + 2);
         to[e] = v;
@@ -932,8 +944,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(Mer
   }
   if constexpr (W == 1) {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) store_y(Y + (size_t)row * D + lane + 64 * i, l == 0.f ? 0.f : o[i] / l);
-    if (lane == 0 && LSE) LSE[row] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    for (int i = 0; i < EPL; ++i) store_y(Y + (size_t)row * D + lane + 64 * i, weighted_mean(o[i], l));
+    if (lane == 0 && LSE) LSE[row] = log_of_sum(m, l);
     return;
   }
 #pragma unroll
@@ -954,8 +966,8 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(Mer
       sum = fmaf(f, lds_l[w], sum);
       v = fmaf(f, lds_o[w][e], v);
     }
-    store_y(Y + (size_t)row * D + e, sum == 0.f ? 0.f : v / sum);
-    if (e == 0 && LSE) LSE[row] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+    store_y(Y + (size_t)row * D + e, weighted_mean(v, sum));
+    if (e == 0 && LSE) LSE[row] = log_of_sum(M, sum);
   }
 }
 

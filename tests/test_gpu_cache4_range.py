@@ -1,5 +1,7 @@
 """Attention over the cache held in 4 bits (sa_cache4_decode_fwd) at the ends of its range: values of V, scores and queries of any size.  Bounds
 are those of tests/test_gpu_cache4.py unless a test says otherwise."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -102,3 +104,60 @@ def test_scores_of_any_size(dtype, d, size):
         want = float(k[0, 0, row, 5]) * float(q[0, 0, 0, 5])
         assert (np.abs(Y[0, :, 0] - Vr[0, 0, row]) <= (half + 1.01 * p) * np.abs(Vr[0, 0, row])).all(), (rows, Y[0, 0, 0, :4], Vr[0, 0, row, :4])
         assert (np.abs(L / want - 1) <= 2.0 ** -21).all(), (rows, L, want)
+
+
+# ---- queries ------------------------------------------------------------------------------------------------------------------
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T,n", [(1, 1), (1, 40), (3, 40), (1, 9000), (40, 2000)])
+@pytest.mark.parametrize("what", ["infinity", "overflow"])
+def test_scores_that_are_all_below_every_number(dtype, T, n, what):
+    """Softmax over scores that are all -infinity is 0/0, not that of a query without rows; rows of other heads, and queries that see nothing,
+    are as they were"""
+    c = Setup(2, 4, 2, 64, 32, -(-n // 32), dtype, seed=n)
+    K, V = c.rows(n)[0], c.rows(n)[0]
+    K[..., 9] = -4 if what == "infinity" else -2.0 ** 100
+    table = c.dev(c.table)
+    short = min(T, n) - 1                  # the second sequence: its first tokens see nothing
+    sa().sa_cache4_write(c.desc, K, V, None, None, table, c.pool)
+    q = c.dev(c.rng.standard_normal((2, 4, T, 64)).astype(np.float32))
+    q[..., 9] = 0
+    _, Y, L = c.decode(T, [n, short], q=q)
+    q[:, 1, :, 9] = math.inf if what == "infinity" else 2.0 ** 100
+    _, Y2, L2 = c.decode(T, [n, short], q=q)
+    assert np.isnan(Y2[0, 1]).all() and np.isnan(L2[0, 1]).all()
+    sees = T - short
+    assert np.isnan(Y2[1, 1, sees:]).all() and np.isnan(L2[1, 1, sees:]).all()
+    assert (Y2[1, 1, :sees] == 0).all() and np.isneginf(L2[1, 1, :sees]).all()
+    assert np.array_equal(Y[:, 2:], Y2[:, 2:]) and np.array_equal(L[:, 2:], L2[:, 2:])
+    # the head that shares tiles: its maximum is raised elsewhere, weights and sums are rounded anew
+    p, half = (2.0 ** -11, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -22, 2.0 ** -24)
+    tol = 2 * half * np.abs(Y[:, 0]) + 2 * (p + 2 * n * 2.0 ** -24 + 2.0 ** -18) * 1.2 * float(V.abs().max())
+    assert (np.abs(Y[:, 0] - Y2[:, 0]) <= tol).all() and np.array_equal(np.isneginf(L[:, 0]), np.isneginf(L2[:, 0]))
+
+
+@pytest.mark.parametrize("T,n", [(1, 9000), (3, 100)])
+def test_some_scores_below_every_number(T, n):
+    """Rows whose score is -infinity weigh nothing beside others: as if their pages were not there"""
+    c = Setup(1, 4, 2, 128, 32, -(-n // 32), "f32", seed=n)
+    K, V = c.rows(n)[0], c.rows(n)[0]
+    K[..., 9] = 0
+    K[:, :, 32:96, 9] = -2.0 ** 100        # two whole pages
+    sa().sa_cache4_write(c.desc, K, V, None, None, c.dev(c.table), c.pool)
+    q = c.dev(c.rng.standard_normal((1, 4, T, 128)).astype(np.float32))
+    q[..., 9] = 2.0 ** 100
+    _, Y, L = c.decode(T, [n], q=q)
+    table = c.table.copy()
+    table[0, 1:3] = -1
+    _, Y2, L2 = c.decode(T, [n], q=q, table=table)
+    assert np.array_equal(Y, Y2) and np.array_equal(L, L2) and np.isfinite(Y).all()
+
+
+def test_pages_that_are_not_there_leave_nothing_to_see():
+    """Also where the first rows of a sequence would be in sight"""
+    c = Setup(1, 4, 2, 64, 32, 300, "bf16", seed=2)
+    table = np.full_like(c.table, -1)
+    for T in (1, 3, 20):
+        _, Y, L = c.decode(T, [9600], table=table)
+        assert (Y == 0).all() and np.isneginf(L).all()
