@@ -535,6 +535,22 @@ __device__ __forceinline__ void load_q8<float>(const float* p, float (&x)[8]) {
 __device__ __forceinline__ void store_y(bf16_t* p, float v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
 __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 
+// fp32 elements x and y of q as three numbers of 8 bits.  The first of one past bf16's largest is that and not the infinity to which it would be
+// rounded: 16 bits remain for the others.  An infinity stays one.
+__device__ __forceinline__ float within_bf16(float x) {
+  const float top = __uint_as_float(0x7f7f0000u);
+  return fabsf(x) < INFINITY ? fminf(fmaxf(x, -top), top) : x;
+}
+template <int PARTS>
+__device__ __forceinline__ void split_query(float x, float y, uint32_t* w) {
+  if constexpr (PARTS == 1) {
+    w[0] = pack_bf16(x, y);
+  } else {
+    w[0] = pack_bf16(within_bf16(x), within_bf16(y));
+    split_pair_bf16<PARTS - 1>(x - bf16lo(w[0]), y - bf16hi(w[0]), w + 1);
+  }
+}
+
 // The lane's part of its query rows (past the last: that one again) as operands
 template <typename T, int D, int NT, int QP>
 __device__ __forceinline__ void load_queries(const T* q, int row0, int rows, int r, int g, bf16x8 (&qf)[NT][D / 32][QP]) {
@@ -549,7 +565,7 @@ __device__ __forceinline__ void load_queries(const T* q, int row0, int rows, int
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         uint32_t p[QP];
-        split_pair_bf16<QP>(x[2 * i], x[2 * i + 1], p);
+        split_query<QP>(x[2 * i], x[2 * i + 1], p);
 #pragma unroll
         for (int k = 0; k < QP; ++k) w[k][i] = p[k];
       }

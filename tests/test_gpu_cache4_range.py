@@ -6,6 +6,7 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import cache4 as orc
 from tests import gpu_util as U
 from tests.test_gpu_cache4 import Setup, sa
 
@@ -161,3 +162,22 @@ def test_pages_that_are_not_there_leave_nothing_to_see():
     for T in (1, 3, 20):
         _, Y, L = c.decode(T, [9600], table=table)
         assert (Y == 0).all() and np.isneginf(L).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("T", [1, 20])
+def test_fp32_queries_next_to_the_largest_number(d, T):
+    """Past bf16's largest number their first part of 8 bits is that one, and all three add up to the number as ever"""
+    c = Setup(1, 4, 2, d, 32, 4, "f32", seed=d)
+    c.write(c.rows(100, 2.0 ** -124), c.rows(100))
+    q = c.rng.uniform(-1, 1, (1, 4, T, d)) * 2.0 ** 121
+    top = float(np.finfo(np.float32).max)
+    q[..., 3] = top
+    q[..., 7] = -top * (1 - 2.0 ** -20)
+    q[..., 11] = 3.3895e38                 # the first that is rounded up to an infinity is 3.3961e38
+    q = c.dev(q.astype(np.float32))
+    _, Y, L = c.decode(T, [100], q=q)
+    Yr, Lr, A = orc.attention(c.oracle, c.table, U.to_np64(q), [100], 100, c.scale)
+    delta = (d + 8) * 2.0 ** -24 * A + 2.0 ** -22 * (1 + A)
+    assert (np.abs(Y - Yr) <= 2.0 ** -24 * np.abs(Yr) + ((2 * delta + 2.0 ** -22 + 200 * 2.0 ** -24) * c.vmax)[..., None]).all()
+    assert (np.abs(L - Lr) <= delta + 100 * 2.0 ** -24 + 2.0 ** -22 * (1 + np.abs(Lr))).all()
