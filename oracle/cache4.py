@@ -30,6 +30,20 @@ def value(code: int, byte: int) -> float:
     return (-1.0 if code & 8 else 1.0) * MAGNITUDES[code & 7] * 2.0 ** (byte - 127)
 
 
+def blocks_held(x):
+    """Many blocks at once, fp64 [n, 32] -> the values that they are held as: of the two magnitudes next to an element the nearer, of two equally
+    near ones that of the even code (0, 1, 2, 4)"""
+    grid = np.array(MAGNITUDES)
+    top = np.abs(x).max(1)
+    e = np.frexp(np.where(top > 0, top, 1))[1] - 3
+    e = np.where(top > 0, np.clip(e + (top / 2.0 ** e > 7), -125, 125), 0)
+    v = np.minimum(np.abs(x) / 2.0 ** e[:, None], 6)
+    low = np.clip(np.searchsorted(grid, v, side="right") - 1, 0, 6)
+    below, above = v - grid[low], grid[low + 1] - v
+    code = np.where(below < above, low, np.where(below > above, low + 1, low + (low & 1)))
+    return np.copysign(grid[code] * 2.0 ** e[:, None], x)
+
+
 def quantise_row(k, v):
     """One row of K and of V of one head -> (codes, bytes) of each"""
     bad = not (np.isfinite(k).all() and np.isfinite(v).all())

@@ -49,6 +49,19 @@ def test_the_largest_numbers_are_held_as_numbers():
         assert e == 125 and orc.value(orc.element_code(amax, e), e + 127) == 6 * 2.0 ** 125
 
 
+@pytest.mark.parametrize("spread", [0, 1, 3, 30, 120])
+def test_blocks_at_once_and_element_by_element(spread):
+    rng = np.random.default_rng(spread)
+    x = rng.choice([-1, 1], (200, 32)) * (1 + rng.integers(0, 128, (200, 32)) / 128) * 2.0 ** rng.integers(-126 + spread, 128 - spread // 2, (200, 1))
+    x = x.astype(np.float32).astype(np.float64) * 2.0 ** -rng.integers(0, spread + 1, (200, 32)).astype(np.float64)
+    x[rng.random(x.shape) < 0.1] = 0
+    x[0], x[1, 1:], x[2] = 0, 0, -0.0
+    e = [orc.block_exponent(np.abs(b).max()) for b in x]
+    want = np.array([[orc.value(orc.element_code(v, k), k + 127) for v in b] for b, k in zip(x, e)])
+    got = orc.blocks_held(x)
+    assert np.array_equal(got, want) and np.array_equal(np.signbit(got), np.signbit(want))
+
+
 @pytest.mark.parametrize("d", [64, 128])
 def test_every_byte_of_a_tile_has_one_place(d):
     c = orc.Cache(1, d, 32, 1)
