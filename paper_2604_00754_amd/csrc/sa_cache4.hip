@@ -381,11 +381,10 @@ struct MergeArgs {
 // kNone: the maximum before a row has been seen, the lowest number (a row that is not seen has the score -inf).
 constexpr float kRaise = 8.f, kLift = 7.f, kNone = -3.402823466e38f;
 
-// A query's sum of weights is 0 where it sees nothing and at least 2^-50 where it sees a number; kAllBelow and its multiples stand for rows whose scores
-// are all -inf, beside which any number counts alone and whose own softmax is 0/0.
-constexpr float kAllBelow = 0x1p-126f, kSomething = 0x1p-100f;
-__device__ __forceinline__ float weighted_mean(float v, float sum) { return sum == 0.f ? 0.f : sum < kSomething ? __uint_as_float(0x7fc00000u) : v / sum; }
-__device__ __forceinline__ float log_of_sum(float m, float sum) { return sum == 0.f ? -INFINITY : sum < kSomething ? __uint_as_float(0x7fc00000u) : (m + log2f(sum)) * kLn2; }
+// A query that sees nothing has the maximum -inf; one whose scores are all -inf kNone and a sum of 0, which beside any number counts for nothing and by
+// itself leaves 0/0.
+__device__ __forceinline__ float weighted_mean(float m, float v, float sum) { return m == -INFINITY ? 0.f : v / sum; }
+__device__ __forceinline__ float log_of_sum(float m, float sum) { return sum == 0.f ? (m == -INFINITY ? m : __uint_as_float(0x7fc00000u)) : (m + log2f(sum)) * kLn2; }
 
 __device__ __forceinline__ float exp2_above(float a, float ref) { return exp2f(a - (ref == -INFINITY ? 0.f : ref)); }
 
@@ -839,8 +838,14 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     lift = bf16_lift(most_byte, len);
     walk(bf16x8{});
   }
+  int sight = 0x7fffffff;  // the first position of the first of the wave's tiles that is there
 #pragma unroll
-  for (int n = 0; n < NT; ++n) m[n] -= lift;  // what the sums are relative to
+  for (int k = kLists - 1; k >= 0; --k) {
+    const unsigned long long there = __ballot(numbers[k] >= 0);
+    sight = there ? (first + W * (64 * k + (int)__builtin_ctzll(there))) * kTile : sight;
+  }
+#pragma unroll
+  for (int n = 0; n < NT; ++n) m[n] = last[n] < sight ? -INFINITY : m[n] - lift;  // what the sums are relative to
 
   // the waves' results, 16 query rows at a time
 #pragma unroll
@@ -848,12 +853,6 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
     float ls = l[n];
     ls += __shfl_xor(ls, 16);
     ls += __shfl_xor(ls, 32);
-    if (__any(ls == 0.f && last[n] >= first * kTile)) {  // pages that are not there, or scores that are all -inf
-      bool seen = false;
-#pragma unroll 1
-      for (int i = 0; i < turns; ++i) seen |= number_of(i) >= 0 && (first + W * i) * kTile <= last[n];
-      if (ls == 0.f && seen) ls = kAllBelow;
-    }
     if (n > 0) __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -881,7 +880,7 @@ __global__ __launch_bounds__(W * 64, attn_waves_per_simd(sizeof(T) == 2, D, NT))
       }
       const size_t out = (size_t)bh * a.rows + row;
       if (pieces == 1) {
-        store_y(reinterpret_cast<T*>(a.Y) + out * D + e, weighted_mean(v, sum));
+        store_y(reinterpret_cast<T*>(a.Y) + out * D + e, weighted_mean(M, v, sum));
         if (e == 0 && a.LSE) a.LSE[out] = log_of_sum(M, sum);
       } else {
         float* to = a.part + (((size_t)hk * a.rows + row) * (a.c.B * a.splits) + slot) * (D + 2);
@@ -960,7 +959,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(Mer
   }
   if constexpr (W == 1) {
 #pragma unroll
-    for (int i = 0; i < EPL; ++i) store_y(Y + (size_t)row * D + lane + 64 * i, weighted_mean(o[i], l));
+    for (int i = 0; i < EPL; ++i) store_y(Y + (size_t)row * D + lane + 64 * i, weighted_mean(m, o[i], l));
     if (lane == 0 && LSE) LSE[row] = log_of_sum(m, l);
     return;
   }
@@ -982,7 +981,7 @@ __global__ __launch_bounds__(W == 1 ? 256 : W * 64) void cache4_merge_kernel(Mer
       sum = fmaf(f, lds_l[w], sum);
       v = fmaf(f, lds_o[w][e], v);
     }
-    store_y(Y + (size_t)row * D + e, weighted_mean(v, sum));
+    store_y(Y + (size_t)row * D + e, weighted_mean(M, v, sum));
     if (e == 0 && LSE) LSE[row] = log_of_sum(M, sum);
   }
 }
