@@ -534,18 +534,14 @@ __device__ __forceinline__ void load_q8<float>(const float* p, float (&x)[8]) {
 __device__ __forceinline__ void store_y(bf16_t* p, float v) { *reinterpret_cast<uint16_t*>(p) = (uint16_t)(pack_bf16(v, 0.f) & 0xffffu); }
 __device__ __forceinline__ void store_y(float* p, float v) { *p = v; }
 
-// fp32 elements x and y of q as three numbers of 8 bits.  The first of one past bf16's largest is that and not the infinity to which it would be
-// rounded: 16 bits remain for the others.  An infinity stays one.
-__device__ __forceinline__ float within_bf16(float x) {
-  const float top = __uint_as_float(0x7f7f0000u);
-  return fabsf(x) < INFINITY ? fminf(fmaxf(x, -top), top) : x;
-}
+// Elements x and y of q as numbers of 8 bits.  The first of three is cut off, not rounded, so that one past bf16's largest number does not become an
+// infinity: 16 bits remain for the others either way.
 template <int PARTS>
 __device__ __forceinline__ void split_query(float x, float y, uint32_t* w) {
   if constexpr (PARTS == 1) {
     w[0] = pack_bf16(x, y);
   } else {
-    w[0] = pack_bf16(within_bf16(x), within_bf16(y));
+    w[0] = __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302u);
     split_pair_bf16<PARTS - 1>(x - bf16lo(w[0]), y - bf16hi(w[0]), w + 1);
   }
 }
