@@ -360,7 +360,8 @@ sa_status sa_cache4_decode_fwd(const sa_cache4_desc* desc, const void* q, int32_
  * these rows touch and that are not there get free pages, those whose page is shared (count > 1) get a page of their own, into which
  * the shared page is copied, in all layers, if rows below lens[b] lie in it.  Pages are dealt lowest first, in the
  * order of b and position.  info[0] = pages taken; if too few are free nothing is changed, info[0] = 0 and
- * info[1] = pages that lack (0 otherwise).  All sequences are judged by the counts before the call.
+ * info[1] = pages that lack (0 otherwise).  All sequences are judged by the counts before the call: each that shares a page with others gets one of its
+ * own, and if all of them do the shared one is free afterwards (so as many pages are needed for that as sequences, not one less).
  *
  * sa_pages_compact moves pages in use to the front: with U pages in use, the highest of them goes to the lowest free page,
  * and so on until all lie below U or max_moves pages have moved.  Pages move in all layers; table entries and counts

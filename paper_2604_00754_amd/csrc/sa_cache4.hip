@@ -351,7 +351,7 @@ __global__ __launch_bounds__(kRowWaves * 64) void cache4_read_kernel(RowsArgs a)
 // f16's reach the wave's tiles are gone through again in bf16 with a part more.
 // Bound.  One token: the K/V rows once, d + d/16 bytes a row, HBM: 16 x 8192 rows of 8 KV heads of 128 (143 MB) 31 us with the
 // merge, the kernel itself 5.3 TB/s; a tile is 184 vector instructions, which bound the chip at 11 TB/s.  Many tokens: the vector ALU
-// (T509 over 32768 rows, 32 / 8 heads 296 us, 0.92 PFLOP/s: active in 88 % of the waves' cycles, the matrix pipe in 44 %): of 254 instructions for 32 query rows
+// (T509 over 32768 rows, 32 / 8 heads 296 us, 0.92 PFLOP/s: active in 87 % of the waves' cycles, the matrix pipe in 43 %): of 254 instructions for 32 query rows
 // half unpack the tile.  Sharing that over the waves of a workgroup through LDS left 150 and took as long, LDS reads and barriers in
 // its place; 48 rows a wave 302 us, 64 rows 433 (one wave a SIMD).
 struct AttnArgs {
@@ -1024,8 +1024,8 @@ Plan pieces_plan(const sa_cache4_desc* c, int T, long tiles) {
   }
   // Bound by the vector ALU.  The launch is as many workgroups at a time as fit the chip, each a piece's tiles long and what a prologue and an
   // end take, about six; with k waves a SIMD all of that takes 1 + 0.6 (k - 1) times as long as with one; joining pieces takes about
-  // eight.  The least of that for pieces that fill one, two, .. waves a SIMD, and two and three such rounds (us, pieces of one / two waves:
-  // T5, B4 x 8192 rows, 32 / 8 heads 15.4 / 17.7; T128 over 32768 rows 95 / 79; T509 over 32768 rows in two and a part rounds 295, in two 275).
+  // eight.  The least of that for pieces that fill one, two, .. waves a SIMD, and two and three such rounds (us, pieces of one wave / two / four: T5,
+  // B4 x 8192 rows, 32 / 8 heads 15.8 / 17.7 / 25.0; T128 over 32768 rows 98.8 / 85.8 / 92.0; T509 over 32768 rows in two rounds 298, in three or four 305).
   const int per_simd = attn_waves_per_simd(c->dtype == SA_BF16, c->d, p.nt);
   const long fit = 256 * per_simd;  // (a workgroup is a wave on each SIMD)
   p.splits = least;
