@@ -78,10 +78,11 @@ def test_large_values_of_v_and_scores_that_rise(dtype):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("size", [2.0 ** 20, 2.0 ** 29, 2.0 ** 33, 2.0 ** 60, 2.0 ** 120, 1.3125 * 2.0 ** 126, -1.3125 * 2.0 ** 127, -2.0 ** 60, -2.0 ** 33, -2.0 ** 29])
-def test_scores_of_any_size(dtype, d, size):
+@pytest.mark.parametrize("heads", [2, 40])
+def test_scores_of_any_size(dtype, d, size, heads):
     """One element of q meets one of K, so that scores are single products k * size, far enough apart that one row takes all: its V comes back, to
     the product's rounding of a weight (2^-11, 2^-22) that the sum takes whole, and the result's."""
-    c = Setup(1, 2, 1, d, 32, 12, dtype, seed=3, scale=1.0)
+    c = Setup(1, heads, 1, d, 32, 12, dtype, seed=3, scale=1.0)
     n = 384
     k = np.zeros((1, 1, n, d), np.float32)
     grid = np.float32([0.5, 1, 1.5])
@@ -96,7 +97,7 @@ def test_scores_of_any_size(dtype, d, size):
         k *= 0.25 if size > 0 else 2
     c.write(held(c, k), c.rows(n))
     _, Vr = c.read(n, None, None)
-    q = torch.zeros(1, 2, 1, d, device=U.DEV)
+    q = torch.zeros(1, heads, 1, d, device=U.DEV)
     q[..., 5] = size
     q = q.to(U.tdtype(dtype))
     p, half = (2.0 ** -11, 2.0 ** -8) if dtype == "bf16" else (2.0 ** -22, 2.0 ** -24)
