@@ -6,6 +6,7 @@
 #include <initializer_list>
 #include <mutex>
 
+#include "sa_cache4.h"
 #include "sa_common.h"
 
 namespace {

@@ -5,7 +5,7 @@
 // exactly, and what rounding there is lies in q (none in bf16), in the probabilities and in the sums.
 #include <math.h>
 
-#include "sa_common.h"
+#include "sa_cache4.h"
 #include "sa_mfma.h"
 
 namespace sa {

@@ -2,7 +2,7 @@
 // moving the pages in use to the front.  Tables are small and what is decided about them hangs together: one workgroup
 // decides, in a fixed order, and leaves a list; a second launch moves the bytes, at the rate of a copy.  No
 // result depends on the order of anything: counts change by integer atomics, pages are dealt by prefix sums.
-#include "sa_common.h"
+#include "sa_cache4.h"
 #include "sa_device.h"
 
 namespace sa {

@@ -24,6 +24,14 @@ def test_traffic_records_parse_and_are_plausible():
         assert source
 
 
+def test_traffic_records_are_of_the_sources_in_this_tree():
+    """A change of a kernel's sources asks for its counters to be read again, a change elsewhere (declarations of other kernels) for another file"""
+    b = load_bench()
+    for op, wl in (("sa_fwd", "qwen3_8b_prefill_32k"), ("sa_bwd", "qwen3_8b_prefill_32k"), ("sa_bwd", "pretrain_fwdbwd_8k"), ("gated_sa_swa_fwd", "pretrain_fwdbwd_8k")):
+        nbytes, source = b.measured_traffic(op, wl)
+        assert nbytes is not None and nbytes > 0, source
+
+
 def test_traffic_is_withheld_when_a_kernel_source_changes(tmp_path):
     b = load_bench()
     shutil.copytree(b.CSRC, tmp_path / "csrc", ignore=shutil.ignore_patterns("*.o", "*.tmp"))
